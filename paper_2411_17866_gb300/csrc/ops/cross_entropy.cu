@@ -342,7 +342,7 @@ struct EpiLoss {
             for (int k = 1; k < 32; ++k) most = fmaxf(most, v[k]);
             most = fmaxf(top, most);
             const float ref = reference(most);
-            sum *= exp2_fast(reference(top) - ref);
+            sum *= rescale(top, ref);
             float part[4] = {};
 #pragma unroll
             for (int k = 0; k < 32; ++k) part[k % 4] += exp2_fast(fmaf(v[k], kLog2e, -ref));

@@ -25,10 +25,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // later changes of it are exact.
 __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : rintf(top * kLog2e); }
 
+// What takes a sum over logits up to `top` to the reference `ref` of a larger one.  0 for a sum of nothing (top = -infinity),
+// however far below zero the logits lie: its own reference of 0 would make 2^-ref of it, infinite below logits of -88.
+__device__ __forceinline__ float rescale(float top, float ref) { return exp2_fast(rintf(top * kLog2e) - ref); }
+
 // (largest logit, sum of 2^(s log2(e) - reference)) of two parts.
 __device__ __forceinline__ float2 joined(float2 a, float2 b) {
     const float top = fmaxf(a.x, b.x), ref = reference(top);
-    return make_float2(top, fmaf(a.y, exp2_fast(reference(a.x) - ref), b.y * exp2_fast(reference(b.x) - ref)));
+    return make_float2(top, fmaf(a.y, rescale(a.x, ref), b.y * rescale(b.x, ref)));
 }
 __device__ __forceinline__ float log_sum(float2 v) { return v.x + kLn2 * (log2f(v.y) + fmaf(-kLog2e, v.x, reference(v.x))); }
 
