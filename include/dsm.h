@@ -543,6 +543,12 @@ int dsm_orthogonalize(const dsm_orthogonalize_args* args, void* workspace, size_
  * inputs.  dh and dW have the type dtype and are written whole (not added
  * to); either may be NULL and is then not computed.  tokens = 0 is valid (dW
  * is then 0).
+ * Accuracy of f32 results, each relative to the sum of the sizes of what it
+ * adds up: loss and lse 2^-20 of a logit's products, a row of dh or dW 2^-21
+ * of its own products besides what that makes of the probabilities.  G and h
+ * keep this down to 2^-17 of the largest value of their token (for dh) or of
+ * all tokens (for dW), and 2^-39 of that absolutely; the size of a row of W or
+ * h costs no other row anything.  bf16: G and the results are rounded to bf16.
  * Nothing of the size tokens x vocab is kept: the loss' workspace holds 8
  * bytes for a token and 128 rows of W (64 with 32-bit operands), the
  * gradient's a piece of the vocabulary for all tokens, at most 256 MB (512

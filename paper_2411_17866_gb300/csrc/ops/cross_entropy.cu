@@ -13,9 +13,13 @@
 // the vocabulary where there are few rows) and its rows of dW.
 //
 // Numbers.  16-bit operands are multiplied as they are (bf16, f32 accumulators), G is rounded to bf16.  32-bit operands
-// are kept as pairs hi + lo of f16 (22 bits) and multiplied in three terms; every row of h and of W is scaled by a power
-// of two of its own so that its largest value lies just below f16's range, and G by one for all (with the rows' scales
-// folded in, since G's rows and columns are summed over).  Statistics, lse and the sums for dh are in f32.
+// are kept as pairs hi + lo of f16 (22 bits) and multiplied in three terms.  Every row of h and of W is scaled by a power
+// of two of its own so that its largest value lies just below f16's range.  G is kept twice, because the scales of what its
+// products sum over have to be folded into it: for dh = G W with the scales of W's rows and one of its own for every token;
+// for dW = G^T h with one for all, against h scaled by one for all.  So neither a row of W nor a token sets the
+// precision of another's gradient: values of G and of h keep 22 bits down to 2^-17 of the largest, and 2^-39 of that as an
+// absolute error below.  (G once, with both scales folded in: rows of W or h that are zero, or much smaller than the
+// others, cost dh and dW up to 31 bits.)  Statistics, lse and the sums for dh are in f32.
 #include <type_traits>
 
 #include "few_tokens.cuh"
@@ -29,12 +33,20 @@ constexpr uint32_t kSms = 152;         // of a GB300: what work is divided for
 constexpr uint32_t kRowPad = 256;      // rows of the gathered h and of G come in multiples of this
 constexpr int kTopExponent = 14;       // of the largest value of a scaled row
 
-// floor(log2 v) of a finite v > 0, within the range in which 2^(kTopExponent - it) and its inverse are normal numbers.
+// floor(log2 |v|), within the range in which 2^(kTopExponent - it) and its inverse are normal numbers.
+constexpr int kLeastExponent = kTopExponent - 126;
 __device__ __forceinline__ int exponent(float v) {
     const int e = static_cast<int>(__float_as_uint(v) >> 23 & 255) - 127;
-    return e < -100 ? -100 : e > 120 ? 120 : e;
+    return e < kLeastExponent ? kLeastExponent : e > 127 ? 127 : e;
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+// v 2^e for e in [-252, 254]
+__device__ __forceinline__ float times_power(float v, int e) { return v * power(e / 2) * power(e - e / 2); }
+
+// What 32-bit operands are scaled by: exponents of the largest |grad_loss|, of the largest inverse scales of h and of W.
+struct Scales {
+    int grad, h, w;
+};
 
 // 16-bit operand planes of rows of h or W: bf16, or f16 pairs with the inverse of every row's scale.
 struct Planes {
@@ -43,9 +55,10 @@ struct Planes {
     uint32_t ld;              // a multiple of 8
 };
 
-// One row, by one warp.  Returns the inverse of its scale (1 for bf16).
+// One row, by one warp.  Returns the exponent of the inverse of its scale (0 for bf16); a row of zeros has the least one, so
+// that it is nobody's largest.
 template <typename T>
-__device__ __forceinline__ float copy_row(const T* src, uint32_t width, const Planes& to, uint64_t row, uint32_t lane) {
+__device__ __forceinline__ int copy_row(const T* src, uint32_t width, const Planes& to, uint64_t row, uint32_t lane) {
     const uint64_t at = row * to.ld;
     constexpr bool kPair = sizeof(T) == 4;
     const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
@@ -59,7 +72,8 @@ __device__ __forceinline__ float copy_row(const T* src, uint32_t width, const Pl
             for (int i = 0; i < 8; ++i) v[i] = k + i < width ? src[k + i] : round_to<T>(0.f);
         }
     };
-    float scale = 1.f, inverse = 1.f;
+    float scale = 1.f;
+    int inverse = 0;
     if constexpr (kPair) {
         float most = 0.f;
 #pragma unroll 2
@@ -73,11 +87,9 @@ __device__ __forceinline__ float copy_row(const T* src, uint32_t width, const Pl
             }
         }
         most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-        if (most > 0.f) {
-            scale = power(kTopExponent - exponent(most));
-            inverse = power(exponent(most) - kTopExponent);
-        }
-        if (lane == 0) to.inverse[row] = inverse;
+        inverse = exponent(most) - kTopExponent;   // (of 0: the least)
+        scale = most > 0.f ? power(-inverse) : 1.f;
+        if (lane == 0) to.inverse[row] = power(inverse);
     }
 #pragma unroll 2
     for (uint32_t k = lane * 8; k < to.ld; k += 256) {
@@ -135,9 +147,9 @@ struct GatherArgs {
     int64_t ignore;
     uint32_t tokens, vocab, width, per_block, blocks;
     Planes to;
-    const float* grad_loss;   // null, or for `most`: per CTA the largest |grad_loss| / scale of a kept row
+    const float* grad_loss;   // null, or for `most`: per CTA the largest exponents (of grad_loss, of the inverse scales) of kept rows
     uint64_t grad_stride;
-    float* most;
+    int2* most;
     uint32_t* count;          // kept tokens
     uint32_t* splits;         // null, or for SumPlan::parts()
     SumPlan sum;
@@ -174,7 +186,7 @@ __device__ __forceinline__ uint2 count_kept(const GatherArgs& p, uint32_t first,
 // Gathers the kept rows of h in the order of the tokens, and zeros behind them up to a multiple of kRowPad.  Every CTA
 // counts all targets itself: that takes 64 KB from L2 for 8192 tokens.
 template <typename T>
-__device__ __forceinline__ void gather_rows(const GatherArgs& p, float* tops) {
+__device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
     __shared__ uint2 shared[8];
     const uint32_t first = blockIdx.x * p.per_block, end = min(first + p.per_block, p.tokens);   // (none in the last CTAs of few tokens)
     const uint2 c = count_kept(p, first, shared);
@@ -185,7 +197,7 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, float* tops) {
         if (p.splits) *p.splits = p.sum.parts(c.y);
     }
     uint32_t before = c.x;
-    float most = 0.f;
+    int2 most = make_int2(kLeastExponent, -126);
     for (uint32_t t0 = first; t0 < end; t0 += 32) {
         const uint32_t t = t0 + lane;
         const int64_t y = t < end ? target_of(p, t) : p.ignore;
@@ -204,10 +216,10 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, float* tops) {
             left &= left - 1;
             if (i % 8 != warp) continue;
             const T* src = static_cast<const T*>(p.h) + uint64_t(t0 + at) * p.h_stride;
-            const float inverse = copy_row(src, p.width, p.to, before + i, lane);
+            most.y = max(most.y, copy_row(src, p.width, p.to, before + i, lane));
             if (p.grad_loss) {
-                const float a = fabsf(p.grad_loss[(t0 + at) * p.grad_stride]) * inverse;
-                if (a < INFINITY) most = fmaxf(most, a);
+                const float a = fabsf(p.grad_loss[(t0 + at) * p.grad_stride]);
+                if (a < INFINITY) most.x = max(most.x, exponent(a));
             }
         }
         before += __popc(kept);
@@ -222,7 +234,7 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, float* tops) {
         if (lane == 0) tops[warp] = most;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int i = 1; i < 8; ++i) most = fmaxf(most, tops[i]);
+            for (int i = 1; i < 8; ++i) most = make_int2(max(most.x, tops[i].x), max(most.y, tops[i].y));
             p.most[blockIdx.x] = most;
         }
     }
@@ -233,21 +245,21 @@ struct PackArgs {
     uint64_t stride;
     uint32_t rows, width, blocks;
     Planes to;
-    float* most;              // per CTA the largest inverse scale
+    int* most;                // per CTA the exponent of the largest inverse scale
 };
 
 // W as rows that TMA can read, by `blocks` CTAs.
 template <typename T>
-__device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, float* tops) {
+__device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, int2* tops) {
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    float most = 0.f;
+    int most = -126;
     for (uint32_t r = block * 8 + warp; r < p.rows; r += p.blocks * 8)
-        most = fmaxf(most, copy_row(static_cast<const T*>(p.w) + uint64_t(r) * p.stride, p.width, p.to, r, lane));
+        most = max(most, copy_row(static_cast<const T*>(p.w) + uint64_t(r) * p.stride, p.width, p.to, r, lane));
     if (!p.most) return;
-    if (lane == 0) tops[warp] = most;
+    if (lane == 0) tops[warp].x = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) most = fmaxf(most, tops[i]);
+        for (int i = 1; i < 8; ++i) most = max(most, tops[i].x);
         p.most[block] = most;
     }
 }
@@ -256,37 +268,59 @@ __device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, flo
 // 509 tokens on 10007 x 451, loss and gradient 117 us, 121 with two.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_operands(const __grid_constant__ GatherArgs h, const __grid_constant__ PackArgs w) {
-    __shared__ float tops[8];
+    __shared__ int2 tops[8];
     wait_previous();
     if (blockIdx.x < h.blocks) gather_rows<T>(h, tops);
     else pack_rows<T>(w, blockIdx.x - h.blocks, tops);
 }
 
-struct ScaleArgs {
-    const float *most_h, *most_w;
+struct EvenArgs {
+    const int2* most_h;
+    const int* most_w;
     uint32_t n_h, n_w;
-    float* scale;             // G's scale and its inverse
+    Scales* scales;
+    const uint32_t* count;
+    Planes from, to;          // to.hi: null if not needed
 };
 
-// The scale of G: |G_tv| <= |grad_loss_t|, so with the rows' inverse scales folded in it stays below f16's range.
-__global__ void __launch_bounds__(256) k_ce_scale(const __grid_constant__ ScaleArgs p) {
-    __shared__ uint32_t tops[2];
-    if (threadIdx.x < 2) tops[threadIdx.x] = 0;
+// The scales of a call, and the gathered h once more with one scale for all rows (zeros behind the kept rows again).
+__global__ void __launch_bounds__(256) k_ce_even(const __grid_constant__ EvenArgs p) {
+    __shared__ int tops[3];
+    if (threadIdx.x < 3) tops[threadIdx.x] = -126;
     __syncthreads();
     wait_previous();
-    float h = 0.f, w = 0.f;
-    for (uint32_t i = threadIdx.x; i < p.n_h; i += 256) h = fmaxf(h, p.most_h[i]);
-    for (uint32_t i = threadIdx.x; i < p.n_w; i += 256) w = fmaxf(w, p.most_w[i]);
-    atomicMax(&tops[0], __float_as_uint(h));   // of values >= 0: the order of the bits is theirs
-    atomicMax(&tops[1], __float_as_uint(w));
+    int grad = -126, h = -126, w = -126;
+    for (uint32_t i = threadIdx.x; i < p.n_h; i += 256) {
+        grad = max(grad, p.most_h[i].x);
+        h = max(h, p.most_h[i].y);
+    }
+    if (blockIdx.x == 0)
+        for (uint32_t i = threadIdx.x; i < p.n_w; i += 256) w = max(w, p.most_w[i]);
+    atomicMax(&tops[0], grad);
+    atomicMax(&tops[1], h);
+    atomicMax(&tops[2], w);
     __syncthreads();
-    if (threadIdx.x == 0) {
-        h = __uint_as_float(tops[0]);
-        w = __uint_as_float(tops[1]);
-        int e = h > 0.f && w > 0.f ? kTopExponent - exponent(h) - exponent(w) : 0;
-        e = e < -120 ? -120 : e > 120 ? 120 : e;
-        p.scale[0] = power(e);
-        p.scale[1] = power(-e);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.scales = Scales{tops[0], tops[1], tops[2]};
+    if (!p.to.hi) return;
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, count = *p.count;
+    const uint32_t pad = (count + kRowPad - 1) / kRowPad * kRowPad;
+    for (uint32_t r = blockIdx.x * 8 + warp; r < pad; r += gridDim.x * 8) {
+        float by = 0.f;
+        if (r < count) {
+            const int e = static_cast<int>(__float_as_uint(p.from.inverse[r]) >> 23) - 127 - tops[1];
+            by = power(e < -126 ? -126 : e);
+        }
+        for (uint32_t k = lane * 8; k < p.to.ld; k += 256) {
+            const uint64_t at = uint64_t(r) * p.to.ld + k;
+            const uint4 hi = *reinterpret_cast<const uint4*>(p.from.hi + at), lo = *reinterpret_cast<const uint4*>(p.from.lo + at);
+            float v[8];
+            unpack8<__half, true>(hi, lo, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= by;
+            const uint4 e = pack8<__half>(v);
+            *reinterpret_cast<uint4*>(p.to.hi + at) = e;
+            *reinterpret_cast<uint4*>(p.to.lo + at) = rest8<__half>(v, e);
+        }
     }
 }
 
@@ -398,16 +432,19 @@ __global__ void __launch_bounds__(1024) k_ce_join(const __grid_constant__ JoinAr
     p.loss[p.token[r]] = lse - p.target_logit[r];
 }
 
-// A piece of G from the logits.  Rows beyond the kept ones are written as zeros: the products over G read them.
+// A piece of G from the logits.  Rows beyond the kept ones are written as zeros: the products over G read them.  With PAIR
+// it is written twice, scaled for dh and for dW.
 template <bool PAIR>
 struct EpiGrad {
     static constexpr uint32_t kBuffer = 4096;
-    CUtensorMap to[2];        // G, the piece's columns
+    CUtensorMap to[PAIR ? 4 : 1];   // G, the piece's columns; PAIR: hi and lo for dh, then for dW
     const uint32_t* count;
     const int *target, *token;
-    const float *lse, *grad_loss, *h_inverse, *w_inverse, *scale;
+    const float *lse, *grad_loss, *h_inverse, *w_inverse;
+    const Scales* scales;
     uint64_t grad_stride;
     uint32_t v0, columns;     // the piece's first vocabulary row and their number
+    int for_h, for_w;         // which of G's forms are needed
     __device__ __forceinline__ void before(const Tile&, uint32_t, uint32_t, const WarpBuffer&) const {}
     template <int COLUMNS, class Columns>
     __device__ __forceinline__ bool tile(const Tile&, uint32_t row, uint32_t col, const Columns& acc, bool, WarpBuffer& buf) const {
@@ -421,8 +458,6 @@ struct EpiGrad {
             ref = PAIR ? lse[tok] : lse[tok] * kLog2e;
             if constexpr (PAIR) by = h_inverse[row + buf.lane];
         }
-        const float fold = PAIR ? a * (by * *scale) : a;
-        using T = std::conditional_t<PAIR, __half, __nv_bfloat16>;
 #pragma unroll
         for (int c = 0; c < COLUMNS; c += 64) {
             const uint32_t c0 = col + c;
@@ -431,27 +466,46 @@ struct EpiGrad {
             acc.load(c + 32, *reinterpret_cast<float(*)[32]>(v + 32));
             if (c + 64 == COLUMNS) acc.done();
             if (c0 >= columns) continue;
+            const float* iw = PAIR ? w_inverse + v0 + c0 : nullptr;
 #pragma unroll
             for (int k = 0; k < 64; ++k) {
-                float iw = 1.f;
-                if constexpr (PAIR) iw = w_inverse[v0 + c0 + k];
                 // (32-bit: the difference first, which is exact where the probability is large)
-                float g = exp2_fast(PAIR ? (v[k] * by * iw - ref) * kLog2e : fmaf(v[k], kLog2e, -ref));
+                float g = exp2_fast(PAIR ? (v[k] * (by * iw[k]) - ref) * kLog2e : fmaf(v[k], kLog2e, -ref));
                 if (y - c0 == k) g -= 1.f;
-                v[k] = in ? g * fold * iw : 0.f;
+                v[k] = !in ? 0.f : PAIR ? g : g * a;
             }
-#pragma unroll
-            for (int part = 0; part < (PAIR ? 2 : 1); ++part) {
+            auto store = [&](const CUtensorMap& map, auto piece) {
                 buf.reuse();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint4 e = pack8<T>(v + 8 * j);
-                    sts128(buf.at(j), part ? rest8<T>(v + 8 * j, e) : e);
-                }
+                for (int j = 0; j < 8; ++j) sts128(buf.at(j), piece(j));
                 if (buf.written()) {
-                    tma_store(&to[part], buf.addr, c0, row, 0);
+                    tma_store(&map, buf.addr, c0, row, 0);
                     tma_store_commit();
                 }
+            };
+            if constexpr (!PAIR) {
+                store(to[0], [&](int j) { return pack8<__nv_bfloat16>(v + 8 * j); });
+            } else {
+                auto both = [&](int first, auto value) {
+                    auto eight = [&](int j, float (&x)[8]) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = value(8 * j + i);
+                    };
+                    float x[8];
+                    store(to[first], [&](int j) {
+                        eight(j, x);
+                        return pack8<__half>(x);
+                    });
+                    store(to[first + 1], [&](int j) {
+                        eight(j, x);
+                        return rest8<__half>(x, pack8<__half>(x));
+                    });
+                };
+                // |G_tv| <= |grad_loss_t|: below f16's range with its exponent taken out
+                const Scales sc = *scales;
+                const float own = a * power(kTopExponent - exponent(a)), all = a * power(kTopExponent - sc.grad), down = power(-sc.w);
+                if (for_h) both(0, [&](int k) { return v[k] * own * (iw[k] * down); });
+                if (for_w) both(2, [&](int k) { return v[k] * all; });
             }
         }
         return true;
@@ -500,17 +554,16 @@ struct EpiWeight {
     CUtensorMap to;           // of the piece's rows, if tma
     T* dw;                    // of the piece's first row
     uint64_t stride;
-    const float *w_inverse, *scale;   // of 32-bit operands
-    uint32_t rows, width, v0;
+    const Scales* scales;     // of 32-bit operands
+    uint32_t rows, width;
     int tma;
     __device__ __forceinline__ void before(const Tile&, uint32_t, uint32_t, const WarpBuffer&) const {}
     template <int COLUMNS, class Columns>
     __device__ __forceinline__ bool tile(const Tile&, uint32_t row, uint32_t col, const Columns& acc, bool empty, WarpBuffer& buf) const {
         constexpr bool kPair = sizeof(T) == 4;
         constexpr int kBox = 128 / sizeof(T), kPer = 16 / sizeof(T);
-        float by = 1.f;
-        if constexpr (kPair)
-            if (row + buf.lane < rows) by = __fdiv_rn(scale[1], w_inverse[v0 + row + buf.lane]);   // powers of two
+        const int e = kPair ? scales->grad + scales->h - kTopExponent : 0;
+        const float by[2] = {power(e / 2), power(e - e / 2)};
 #pragma unroll
         for (int c = 0; c < COLUMNS; c += kBox) {
             float v[kBox];
@@ -523,8 +576,8 @@ struct EpiWeight {
             for (int j = 0; j < 8; ++j) {
                 uint4 r;
                 if constexpr (kPair)
-                    r = make_uint4(__float_as_uint(v[4 * j] * by), __float_as_uint(v[4 * j + 1] * by),
-                                   __float_as_uint(v[4 * j + 2] * by), __float_as_uint(v[4 * j + 3] * by));
+                    r = make_uint4(__float_as_uint(v[4 * j] * by[0] * by[1]), __float_as_uint(v[4 * j + 1] * by[0] * by[1]),
+                                   __float_as_uint(v[4 * j + 2] * by[0] * by[1]), __float_as_uint(v[4 * j + 3] * by[0] * by[1]));
                 else
                     r = pack8<T>(v + kPer * j);
                 sts128(buf.at(j), empty ? uint4{} : r);
@@ -546,7 +599,9 @@ struct EpiWeight {
 
 struct ScatterArgs {
     const int* row;
-    const float *sum, *h_inverse, *scale;
+    const float *sum, *grad_loss;
+    const Scales* scales;     // of 32-bit operands
+    uint64_t grad_stride;
     const uint32_t *count, *splits;
     uint64_t stride;
     uint32_t ld, tokens, width;
@@ -589,11 +644,8 @@ __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ Scat
         if (c >= p.width) continue;
         if constexpr (sizeof(T) == 4) {
             if (row >= 0) {
-                const float by = __fdiv_rn(1.f, p.h_inverse[row]), down = p.scale[1];   // powers of two
-                v.x = v.x * down * by;
-                v.y = v.y * down * by;
-                v.z = v.z * down * by;
-                v.w = v.w * down * by;
+                const int e = exponent(p.grad_loss[t * p.grad_stride]) + p.scales->w - kTopExponent;
+                v = make_float4(times_power(v.x, e), times_power(v.y, e), times_power(v.z, e), times_power(v.w, e));
             }
         }
         __align__(16) T out[4] = {round_to<T>(v.x), round_to<T>(v.y), round_to<T>(v.z), round_to<T>(v.w)};
@@ -614,9 +666,13 @@ __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ Scat
 // Tiles of the products: 256 columns, or 128 where the sums are held in registers (32-bit operands).
 template <bool PAIR>
 constexpr int kTileN = PAIR ? 128 : 256;
+// k between two additions to sums in registers, of 32-bit operands: for dh and dW 64, which keeps a row whose value is a single
+// product (dW's of a target that occurs once) to 3e-7; 128 took it to 7e-7 (loss and gradient of 509 tokens on 10007 x 451: 123.5
+// and 122.9 us).
+constexpr uint32_t kChunkLogits = 128, kChunkGrad = 64;
 constexpr int kPairRows = 128;                   // up to so many tokens a CTA multiplies by itself (CG = 1), else pairs do
 constexpr int kPieceUnit = 256;                  // pieces of the vocabulary come in multiples of this
-constexpr uint64_t kPieceBytes = 256ull << 20;   // most bytes of a piece of G (hi)
+constexpr uint64_t kPieceBytes = 256ull << 20;   // most bytes of a piece of G with 16-bit operands, half of them with 32-bit ones
 
 constexpr uint32_t kGatherBlocks = 512, kPackBlocks = 2048;   // most CTAs of those kernels
 
@@ -641,13 +697,15 @@ struct Plan {
     int tile_v;               // columns of a tile of the logits
     uint32_t groups;          // of the vocabulary's columns, each with a partial result of the loss
     bool pair, pack;          // 32-bit operands; W has to be laid out for TMA
-    Planes h, w;
-    uint16_t* g[2];
+    Planes h, w, even;        // even: h with one scale for all rows
+    uint16_t* g[4];           // hi; hi and lo for dh, for dW
     uint32_t* count;          // kept tokens; parts of dh
     int *target, *token, *row;
     float2* partial;
     float* target_logit;
-    float *most_h, *most_w, *scale;
+    int2* most_h;
+    int* most_w;
+    Scales* scales;
     uint32_t piece, pieces;   // vocabulary rows of a piece of G
     SumPlan parts;            // of dh
     uint32_t splits, ld_sum;  // splits: parts if all tokens are kept
@@ -695,19 +753,24 @@ Plan make_plan(const dsm_linear_ce& p, bool grad, void* workspace) {
         r.w.lo = c.take<uint16_t>(uint64_t(p.vocab) * r.w.ld);
         r.h.inverse = c.take<float>(r.rows);
         r.w.inverse = c.take<float>(round_up(p.vocab, kPieceUnit));
-        r.most_h = c.take<float>(kGatherBlocks);
-        r.most_w = c.take<float>(kPackBlocks);
-        r.scale = c.take<float>(2);
+        r.most_h = c.take<int2>(kGatherBlocks);
+        r.most_w = c.take<int>(kPackBlocks);
+        r.scales = c.take<Scales>(1);
     }
     if (!grad) {
         r.partial = c.take<float2>(uint64_t(r.groups) * r.rows);
         r.target_logit = c.take<float>(r.rows);
     } else {
-        const uint64_t all = round_up(p.vocab, kPieceUnit), most = kPieceBytes / (2 * uint64_t(r.rows));
+        const uint64_t all = round_up(p.vocab, kPieceUnit), most = kPieceBytes / ((r.pair ? 4 : 2) * uint64_t(r.rows));
         r.pieces = most >= all ? 1 : ceil_div(all, most < kPieceUnit ? kPieceUnit : most);
         r.piece = static_cast<uint32_t>(round_up(ceil_div(all, r.pieces), kPieceUnit));
         r.pieces = ceil_div(p.vocab, r.piece);
-        for (int i = 0; i <= r.pair; ++i) r.g[i] = c.take<uint16_t>(uint64_t(r.rows) * r.piece);
+        for (int i = 0; i < (r.pair ? 4 : 1); ++i) r.g[i] = c.take<uint16_t>(uint64_t(r.rows) * r.piece);
+        if (r.pair) {
+            r.even.ld = r.h.ld;
+            r.even.hi = c.take<uint16_t>(uint64_t(r.rows) * r.h.ld);
+            r.even.lo = c.take<uint16_t>(uint64_t(r.rows) * r.h.ld);
+        }
         r.ld_sum = static_cast<uint32_t>(round_up(p.width, 32));
         const uint32_t cg = p.tokens > kPairRows ? 2 : 1, tile_n = r.pair ? kTileN<true> : kTileN<false>;
         r.parts = SumPlan{ceil_div(p.width, tile_n), 128 * cg, kSms / cg, r.piece / kBlockK, tile_n * (r.pair ? 3 : 1), 0};
@@ -735,8 +798,8 @@ int check_args(const char* func, const dsm_linear_ce* p) {
 }
 
 template <typename T>
-cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss, uint64_t grad_stride, uint32_t* status,
-                   cudaStream_t s) {
+cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss, uint64_t grad_stride, bool for_w,
+                   uint32_t* status, cudaStream_t s) {
     GatherArgs a{};
     a.h = p.h;
     a.h_stride = p.h_stride;
@@ -773,7 +836,10 @@ cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss
     }
     const cudaError_t err = launch_grid(k_ce_operands<T>, dim3(a.blocks + k.blocks), 256, 0, s, a, k);
     if (err != cudaSuccess || !scaled) return err;
-    return launch_grid(k_ce_scale, dim3(1), 256, 0, s, ScaleArgs{r.most_h, r.most_w, a.blocks, k.blocks, r.scale});
+    Planes even = r.even;
+    if (!for_w) even.hi = even.lo = nullptr;
+    return launch_grid(k_ce_even, dim3(for_w ? a.blocks : 1), 256, 0, s,
+                       EvenArgs{r.most_h, r.most_w, a.blocks, k.blocks, r.scales, r.count, r.h, even});
 }
 
 // Arguments that both calls check against the device.
@@ -809,9 +875,9 @@ int weight_maps(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_
     return DSM_OK;
 }
 
-int hidden_maps(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_t rows, CUtensorMap (&maps)[2]) {
+int hidden_maps(const char* func, const dsm_linear_ce& p, const Plan& r, const Planes& h, uint32_t rows, CUtensorMap (&maps)[2]) {
     for (int i = 0; i < 2; ++i)
-        if (int rc = make_map(func, &maps[i], i && r.pair ? r.h.lo : r.h.hi, p.width, r.rows, 1, r.h.ld, 0, rows,
+        if (int rc = make_map(func, &maps[i], i && r.pair ? h.lo : h.hi, p.width, r.rows, 1, h.ld, 0, rows,
                               r.pair ? Elem::f16 : Elem::bf16))
             return rc;
     return DSM_OK;
@@ -889,7 +955,7 @@ template <bool PAIR, int CG, int BN = kTileN<PAIR>>
 int forward(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_t* status, int sms, cudaStream_t s) {
     constexpr int kTerms = PAIR ? 3 : 1;
     Maps maps;
-    if (int rc = hidden_maps(func, p, r, 128, maps.a)) return rc;
+    if (int rc = hidden_maps(func, p, r, r.h, 128, maps.a)) return rc;
     if (int rc = weight_maps(func, p, r, 0, p.vocab, BN / CG, maps.b)) return rc;
     Schedule w{};
     w.batches = w.splits = 1;
@@ -902,8 +968,8 @@ int forward(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_t* s
     const uint64_t tiles = uint64_t(w.tiles_m) * w.tiles_n;
     // Sums in registers beyond 512 k: what the accumulators cut off reaches 1e-6 of the loss (width 1600).
     cudaError_t err;
-    if (PAIR || w.k > 512) err = launch_gemm<CG, BN, kTerms, true, !PAIR, false, false>(maps, w, e, tiles, sms, s);
-    else err = launch_gemm<CG, BN, kTerms, PAIR, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    if (PAIR || w.k > 512) err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits : 512, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    else err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits : 0, !PAIR, false, false>(maps, w, e, tiles, sms, s);
     return err == cudaSuccess ? DSM_OK : cuda_fail(func, err, "launch the logits");
 }
 
@@ -920,8 +986,8 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
     base.splits = 1;
     base.status = status;
     CUtensorMap hk[2], hm[2];
-    if (int rc = hidden_maps(func, p, r, 128, hk)) return rc;
-    if (int rc = hidden_maps(func, p, r, 64, hm)) return rc;
+    if (int rc = hidden_maps(func, p, r, r.h, 128, hk)) return rc;
+    if (int rc = hidden_maps(func, p, r, r.pair ? r.even : r.h, 64, hm)) return rc;
     EpiSum es{{}, r.count, r.ld_sum, 0};
     if (int rc = make_map(func, &es.to, r.sum, r.ld_sum, r.parts.rows, 1, r.ld_sum, 0, 32, Elem::f32)) return rc;
     for (uint32_t i = 0; i < r.pieces; ++i) {
@@ -929,13 +995,16 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         CUtensorMap gk[2], gm[2], wk[2], wm[2];
         if (int rc = weight_maps(func, p, r, v0, count, BV / CG, wk)) return rc;
         if (int rc = weight_maps(func, p, r, v0, count, 64, wm)) return rc;
-        EpiGrad<PAIR> eg{{},         r.count,      r.target,    r.token,  lse, grad_loss,
-                         r.h.inverse, r.w.inverse, r.scale, grad_stride, v0,  count};
+        EpiGrad<PAIR> eg{{},        r.count,  r.target,    r.token, lse,   grad_loss,     r.h.inverse,
+                         r.w.inverse, r.scales, grad_stride, v0,      count, dh != nullptr, dw != nullptr};
         for (int k = 0; k < 2; ++k) {
-            const uint16_t* g = r.g[PAIR ? k : 0];
-            if (int rc = make_map(func, &gk[k], g, count, r.rows, 1, r.piece, 0, 128, kElem)) return rc;
-            if (int rc = make_map(func, &gm[k], g, count, r.rows, 1, r.piece, 0, 64, kElem)) return rc;
-            if (int rc = make_map(func, &eg.to[k], g, count, r.rows, 1, r.piece, 0, 32, kElem)) return rc;
+            const uint16_t *for_h = r.g[PAIR ? k : 0], *for_w = r.g[PAIR ? 2 + k : 0];
+            if (int rc = make_map(func, &gk[k], for_h, count, r.rows, 1, r.piece, 0, 128, kElem)) return rc;
+            if (int rc = make_map(func, &gm[k], for_w, count, r.rows, 1, r.piece, 0, 64, kElem)) return rc;
+            if (!PAIR && k) break;
+            if (int rc = make_map(func, &eg.to[k], for_h, count, r.rows, 1, r.piece, 0, 32, kElem)) return rc;
+            if constexpr (PAIR)
+                if (int rc = make_map(func, &eg.to[2 + k], for_w, count, r.rows, 1, r.piece, 0, 32, kElem)) return rc;
         }
         // the piece of G
         Schedule w = base;
@@ -943,7 +1012,7 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         w.tiles_n = ceil_div(count, BV);
         w.k = p.width;
         w.m_count = r.count;
-        err = launch_gemm<CG, BV, kTerms, PAIR, !PAIR, false, false>(Maps{{hk[0], hk[1]}, {wk[0], wk[1]}}, w, eg,
+        err = launch_gemm<CG, BV, kTerms, PAIR ? kChunkLogits : 0, !PAIR, false, false>(Maps{{hk[0], hk[1]}, {wk[0], wk[1]}}, w, eg,
                                                                     uint64_t(w.tiles_m) * w.tiles_n, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the logits' gradient");
         // its contribution to dh
@@ -952,7 +1021,7 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         w.split_count = r.count + 1;
         w.n_fast = 1;
         es.add = i > 0;
-        if (dh) err = launch_gemm<CG, BN, kTerms, PAIR, !PAIR, false, true>(Maps{{gk[0], gk[1]}, {wm[0], wm[1]}}, w, es,
+        if (dh) err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkGrad : 0, !PAIR, false, true>(Maps{{gk[0], gk[1]}, {wm[0], wm[1]}}, w, es,
                                                                             ~uint64_t(0), sms, s);   // (all SMs)
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the gradient of h");
         if (!dw) continue;
@@ -964,16 +1033,17 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         w.k_count = r.count;
         w.n_fast = 1;
         T* out = static_cast<T*>(dw) + uint64_t(v0) * dw_stride;
-        EpiWeight<T> ew{{}, out, dw_stride, r.w.inverse, r.scale, count, p.width, v0, 0};
+        EpiWeight<T> ew{{}, out, dw_stride, r.scales, count, p.width, 0};
         ew.tma = mappable(out, static_cast<int64_t>(dw_stride), 16, count, 1, sizeof(T));
         if (ew.tma)
             if (int rc = make_map(func, &ew.to, out, p.width, count, 1, dw_stride, 0, 32, kOut)) return rc;
-        err = launch_gemm<2, BN, kTerms, PAIR, !PAIR, true, true>(Maps{{gm[0], gm[1]}, {hm[0], hm[1]}}, w, ew,
+        err = launch_gemm<2, BN, kTerms, PAIR ? kChunkGrad : 0, !PAIR, true, true>(Maps{{gm[0], gm[1]}, {hm[0], hm[1]}}, w, ew,
                                                                   uint64_t(w.tiles_m) * w.tiles_n, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the gradient of W");
     }
     if (!p.tokens || !dh) return DSM_OK;
-    ScatterArgs sc{r.row, r.sum, r.h.inverse, r.scale, r.count, r.count + 1, dh_stride, r.ld_sum, p.tokens, p.width, dh};
+    ScatterArgs sc{r.row,       r.sum,    grad_loss, r.scales, grad_stride, r.count, r.count + 1,
+                   dh_stride, r.ld_sum, p.tokens,  p.width,  dh};
     const bool many = r.splits > 8;
     const uint64_t parts = uint64_t(p.tokens) * ceil_div(p.width, 128), blocks = many ? parts : ceil_div(parts, 8);
     const dim3 grid(static_cast<uint32_t>(blocks < 4096 ? blocks : 4096));
@@ -1018,8 +1088,8 @@ extern "C" int dsm_linear_cross_entropy(const dsm_linear_ce* p, float* loss, flo
         const cudaError_t e = p->dtype == DSM_BF16 ? few<__nv_bfloat16>(a, r.few, false, sms, s) : few<float>(a, r.few, false, sms, s);
         return e == cudaSuccess ? DSM_OK : cuda_fail(func, e, "launch the loss of few tokens");
     }
-    cudaError_t err = p->dtype == DSM_BF16 ? gather<__nv_bfloat16>(*p, r, nullptr, 0, status, s)
-                                           : gather<float>(*p, r, nullptr, 0, status, s);
+    cudaError_t err = p->dtype == DSM_BF16 ? gather<__nv_bfloat16>(*p, r, nullptr, 0, false, status, s)
+                                           : gather<float>(*p, r, nullptr, 0, false, status, s);
     if (err != cudaSuccess) return cuda_fail(func, err, "launch the gather");
     if (p->tokens == 0) return DSM_OK;
     const auto go = p->tokens > kPairRows ? (r.pair ? forward<true, 2> : forward<false, 2>)
@@ -1073,8 +1143,8 @@ extern "C" int dsm_linear_cross_entropy_grad(const dsm_linear_ce* p, const float
         return e == cudaSuccess ? DSM_OK : cuda_fail(func, e, "launch the gradient of few tokens");
     }
     cudaError_t err = p->dtype == DSM_BF16
-                          ? gather<__nv_bfloat16>(*p, r, grad_loss, grad_loss_stride, status, s)
-                          : gather<float>(*p, r, grad_loss, grad_loss_stride, status, s);
+                          ? gather<__nv_bfloat16>(*p, r, grad_loss, grad_loss_stride, dw != nullptr, status, s)
+                          : gather<float>(*p, r, grad_loss, grad_loss_stride, dw != nullptr, status, s);
     if (err != cudaSuccess) return cuda_fail(func, err, "launch the gather");
     const auto go = p->tokens > kPairRows ? (r.pair ? backward<true, 2> : backward<false, 2>)
                     : r.pair                ? backward<true, 1>

@@ -14,8 +14,8 @@
 // Three-term products (TERMS = 3): operands kept as pairs hi + lo of 16 bits multiply as lo B_hi + hi B_lo + hi B_hi, from
 // one load of the four tiles.  What is left out (lo B_lo) is 2^-22 of the product in f16 and 2^-16 in bf16.  The tensor
 // cores cut off what falls below the accumulator's last bit, which over a long K adds up to more than these products
-// lose (f16 pairs, Newton-Schulz on 1024 x 4096: 3.6e-5 of the result after five steps).  With CHUNKED the accumulator
-// is added to sums in registers after every 128 k (512 with one term), rounded to nearest, and starts again from zero.
+// lose (f16 pairs, Newton-Schulz on 1024 x 4096: 3.6e-5 of the result after five steps).  With a CHUNK the accumulator
+// is added to sums in registers after every CHUNK of k, rounded to nearest, and starts again from zero.
 #pragma once
 
 #include "dsm_device.cuh"
@@ -49,13 +49,13 @@ struct Tile {
     uint32_t k0, k1;             // blocks of k, a stage each: none if k0 = k1 (the accumulator is then zero)
 };
 
-// CHUNKED: sums in registers.
-template <int CG_, int BN_, int TERMS_, bool CHUNKED_, bool BF16_, uint32_t BUFFER>
+// CHUNK: k between two additions to sums in registers; 0: none.
+template <int CG_, int BN_, int TERMS_, uint32_t CHUNK, bool BF16_, uint32_t BUFFER>
 struct Shape {
     static constexpr int CG = CG_, BN = BN_, TERMS = TERMS_;
-    static constexpr bool CHUNKED = CHUNKED_, BF16 = BF16_;
+    static constexpr bool CHUNKED = CHUNK > 0, BF16 = BF16_;
     static constexpr int kPair = TERMS == 3 ? 2 : 1;
-    static constexpr uint32_t kChunk = TERMS == 3 ? 2 : 8;   // stages between two additions to the register sums
+    static constexpr uint32_t kChunk = CHUNK / kBlockK;      // stages between two additions to the register sums
     // Blocks of 64 k per stage: two where issuing takes longer than multiplying (waits are per stage).
     static constexpr uint32_t kSub = CG == 1 && TERMS == 1 && BN <= 128 ? 2 : 1;
     static constexpr int kEpiWarps = BN == 64 ? 4 : 8;
@@ -405,7 +405,7 @@ struct Pipe {
     }
 };
 
-// Accumulators are handed over in turns: one turn is a tile, or with CHUNKED a chunk of its k (one turn at least).
+// Accumulators are handed over in turns: one turn is a tile, or with a CHUNK that part of its k (one turn at least).
 template <class S>
 __device__ __forceinline__ uint32_t turn_end(const Tile& w, uint32_t k) {
     return !S::CHUNKED || w.k1 - k <= S::kChunk ? w.k1 : k + S::kChunk;

@@ -137,9 +137,9 @@ cudaError_t launch_together(void (*kernel)(Params...), uint64_t clusters, int cl
     return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
 
-template <int CG, int BN, int TERMS, bool CHUNKED, bool BF16, bool A_MN, bool B_MN, class Epi>
+template <int CG, int BN, int TERMS, uint32_t CHUNK, bool BF16, bool A_MN, bool B_MN, class Epi>
 cudaError_t launch_gemm(const Maps& maps, const Schedule& work, const Epi& epi, uint64_t tiles, int sms, cudaStream_t s) {
-    using S = Shape<CG, BN, TERMS, CHUNKED, BF16, Epi::kBuffer>;
+    using S = Shape<CG, BN, TERMS, CHUNK, BF16, Epi::kBuffer>;
     auto kernel = k_gemm<S, A_MN, B_MN, Epi>;
     // per device and cheap (a table lookup in the runtime): not remembered
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);

@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_orth_steps(const __grid_cons
 template <int CG, int BN, bool PAIR, bool TALL>
 int steps(const dsm_orthogonalize_args& p, const Plan& r, uint32_t* status, int dev, cudaStream_t s) {
     using T = std::conditional_t<PAIR, float, __nv_bfloat16>;
-    using S = Shape<CG, BN, PAIR ? 3 : 1, PAIR, false, EpiApply<T>::kBuffer>;
+    using S = Shape<CG, BN, PAIR ? 3 : 1, PAIR ? 128 : 0, false, EpiApply<T>::kBuffer>;
     constexpr uint32_t kBM = 128 * CG, kSquare = kBM > BN ? kBM : BN, kRowsB = BN / CG;
     StepsArgs<PAIR> a{};
     a.to_gram.out.m = a.to_square.out.m = r.m;

@@ -62,3 +62,105 @@ def test_some_logits_far_below_zero(first, last, tokens, dtype):
 def test_logits_far_below_zero_over_a_large_vocabulary(tokens, dtype):
     check_loss(*shifted(tokens, 50257, 64, dtype, -120))
     check_loss(*shifted(tokens, 50257, 64, dtype, -240, slice(7, 40000)))
+
+
+# ---- f32 gradients, row by row, with rows of very different sizes -----------------------------------------------------
+
+def rows_within_bounds(h, w, y, a, **kw):
+    """f32 gradients against 64 bits, every row of dh and of dW by a bound of its own, from the formats alone.
+
+    A logit is known to 2^-20 of the sum of its products' sizes (operands of 22 bits, three terms, f32 sums), and so is its
+    probability; G and h keep 22 bits, and 2^-39 of the largest of a token (for dh) or of all (for dW) as an absolute
+    error; products and sums of f32 add 2^-21 of the sum of their sizes."""
+    kept = y != -100
+    ak = torch.where(kept, a.double().expand(len(y)), 0.0)
+    h64, w64 = torch.where(kept[:, None], h, 0).double(), w.double()
+    p = torch.softmax(h64 @ w64.T, 1)
+    size = (h64.abs() @ w64.abs().T).amax(1).clamp_min(1.0)
+    g = p.clone()
+    g[torch.arange(len(y), device="cuda"), y.clamp_min(0)] -= 1
+    g *= ak[:, None]
+    dh, dw = g @ w64, g.T @ h64
+    off = ak.abs()[:, None] * p * (2.0 ** -20 * size)[:, None] + 2.0 ** -21 * g.abs()
+    wn, hn = w64.norm(dim=1), h64.norm(dim=1)
+    bound_h = off @ wn + 2.0 ** -39 * ak.abs() * len(w) * w.shape[1] ** 0.5 * float(w64.abs().max())
+    bound_w = off.T @ hn + 2.0 ** -39 * float(ak.abs().max()) * hn.sum() \
+        + 2.0 ** -39 * h.shape[1] ** 0.5 * float(h64.abs().max()) * g.abs().sum(0)
+
+    ws = dsm.linear_cross_entropy_workspace(h, w)
+    loss, lse = dsm.linear_cross_entropy(h, w, y, workspace=ws)
+    got_h, got_w = dsm.linear_cross_entropy_grad(h, w, y, lse, a, workspace=ws, **kw)
+    assert dsm.operator_status(ws) == 0
+    assert bool(((got_h.double() - dh).norm(dim=1) <= bound_h).all())
+    assert bool(((got_w.double() - dw).norm(dim=1) <= bound_w).all())
+    return dh, dw, bound_h, bound_w
+
+
+def _sizes(rows, exponents):
+    """A factor of 2^e for three rows of every e."""
+    f = torch.ones(rows, 1, device="cuda")
+    for i, e in enumerate(exponents):
+        f[5 + 7 * i:5 + 7 * i + 3] = 2.0 ** e
+    return f
+
+
+@pytest.mark.parametrize("tokens", [17, 100, 300])
+@pytest.mark.parametrize("what", ["plain", "zero w", "zero h", "zero both", "all w zero", "all h zero", "small w", "small h",
+                                  "small both", "large w", "large h", "spread a", "zero a", "tiny all", "large all"])
+def test_rows_of_different_sizes(what, tokens):
+    h, w, y, a = problem(tokens, 1030, 96, F32, lean=8.0)
+    y[3] = -100
+    if what in ("zero w", "zero both"):
+        w[[0, 400, 1029]] = 0
+    if what in ("zero h", "zero both"):
+        h[[1, 7, tokens - 1]] = 0
+    if what == "all w zero":
+        w.zero_()
+    if what == "all h zero":
+        h.zero_()
+    down, up = (-10, -20, -30, -60, -100), (4, 8)
+    if what in ("small w", "small both"):
+        w *= _sizes(len(w), down)
+    if what in ("small h", "small both"):
+        h *= _sizes(tokens, down)[:tokens]
+    if what == "large w":
+        w *= _sizes(len(w), up)
+    if what == "large h":
+        h *= _sizes(tokens, up)
+    if what == "spread a":
+        a *= 2.0 ** -torch.randint(0, 12, (tokens,), device="cuda")
+    if what == "zero a":
+        a[::2] = 0
+    if what == "tiny all":
+        h, w = h * 2.0 ** 90, w * 2.0 ** -90
+    if what == "large all":
+        h, w, a = h * 2.0 ** -100, w * 2.0 ** 100, a * 2.0 ** 20
+    dh, dw, bound_h, bound_w = rows_within_bounds(h, w, y, a)
+    if what in ("plain", "zero w", "zero h", "zero both", "small w"):
+        # the bounds say something: 1e-4 of a row, for nearly all rows
+        kept = y != -100
+        assert float((bound_h < 1e-4 * dh.norm(dim=1))[kept].double().mean()) > 0.9
+        assert float((bound_w < 1e-4 * dw.norm(dim=1)).double().mean()) > 0.9
+
+
+def test_zero_rows_of_a_larger_problem():
+    """A padding row in W at an odd offset, a zero row among the kept ones, and pieces of the vocabulary."""
+    h, w, y, a = problem(509, 10007, 451, F32, 0.1, lean=8.0)
+    w[17] = 0
+    h[11] = 0
+    y[11] = 5
+    flat = torch.empty(3 + w.numel(), device="cuda")
+    flat[3:] = w.reshape(-1)
+    rows_within_bounds(h, flat[3:].view_as(w), y, a)
+    h, w, y, a = problem(9000, 16000, 24, F32, 0.1)
+    w[[0, 15999]] = 0
+    check(h, w, y, a)
+
+
+def test_one_of_the_gradients_with_rows_of_different_sizes():
+    h, w, y, a = problem(200, 1030, 96, F32)
+    w[:4] = 0
+    _, lse = dsm.linear_cross_entropy(h, w, y)
+    dh, dw = dsm.linear_cross_entropy_grad(h, w, y, lse, a)
+    assert torch.equal(dsm.linear_cross_entropy_grad(h, w, y, lse, a, need_weight=False)[0], dh)
+    assert torch.equal(dsm.linear_cross_entropy_grad(h, w, y, lse, a, need_h=False)[1], dw)
