@@ -548,7 +548,8 @@ int dsm_orthogonalize(const dsm_orthogonalize_args* args, void* workspace, size_
  * of its own products besides what that makes of the probabilities.  G and h
  * keep this down to 2^-17 of the largest value of their token (for dh) or of
  * all tokens (for dW), and 2^-39 of that absolutely; the size of a row of W or
- * h costs no other row anything.  bf16: G and the results are rounded to bf16.
+ * h costs no other row anything.  bf16: G and the results are rounded to bf16;
+ * what W's rows have in common drops out of dh in spite of that.
  * Nothing of the size tokens x vocab is kept: the loss' workspace holds 8
  * bytes for a token and 128 rows of W (64 with 32-bit operands), the
  * gradient's a piece of the vocabulary for all tokens, at most 256 MB (512

@@ -164,3 +164,34 @@ def test_one_of_the_gradients_with_rows_of_different_sizes():
     dh, dw = dsm.linear_cross_entropy_grad(h, w, y, lse, a)
     assert torch.equal(dsm.linear_cross_entropy_grad(h, w, y, lse, a, need_weight=False)[0], dh)
     assert torch.equal(dsm.linear_cross_entropy_grad(h, w, y, lse, a, need_h=False)[1], dw)
+
+
+# ---- rows of W that share a direction ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [1, 3, 16, 100, 300])
+@pytest.mark.parametrize("shift", [-56, -88, -96, -120, -400])
+def test_gradients_where_all_rows_share_a_direction(shift, tokens, dtype):
+    """The gradient of the logits adds up to zero over the vocabulary, so what W's rows have in common is not in dh."""
+    check(*shifted(tokens, 1030, 96, dtype, shift))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [1, 60, 200])
+def test_gradients_where_rows_of_a_large_vocabulary_share_a_direction(tokens, dtype):
+    check(*shifted(tokens, 50257, 64, dtype, -120))
+    check(*shifted(tokens, 50257, 64, dtype, -240, slice(7, 40000)))
+
+
+def test_gradients_where_all_rows_share_a_direction_by_pieces_and_parts():
+    """Sums over a row of G that several pieces of the vocabulary and several parts of it add to, with ignored tokens, W at
+    an odd offset, and a gradient of one token far smaller than the others'."""
+    h, w, y, a = shifted(9000, 33001, 64, BF16, -120)
+    y[::3] = -100
+    check(h, w, y, a)
+    h, w, y, a = shifted(70, 9001, 101, BF16, -120)
+    y[5] = -100
+    a[6], a[7] = 0, 1e-30
+    flat = torch.empty(1 + w.numel(), dtype=BF16, device="cuda")
+    flat[1:] = w.reshape(-1)
+    check(h, flat[1:].view_as(w), y, a)
