@@ -506,7 +506,8 @@ int dsm_operator_status(const void* workspace, dsm_stream_t stream, uint32_t* st
  * steps = 0: only u / max(||u||_F, eps).
  * Accuracy: a bf16 result is within 0.5 % (Frobenius norm) of the formula's
  * value, an f32 result within 1e-5 for matrices that are not nearly of low
- * rank.  A NaN or an infinity in g makes its whole matrix NaN; a zero matrix
+ * rank, for entries of any size (of u: those below 2^-84 count less in the
+ * norm).  A NaN or an infinity in g makes its whole matrix NaN; a zero matrix
  * stays zero.  Sizes of 0 are valid and do nothing. */
 #define DSM_ORTHOGONALIZE_MAX_STEPS 64
 typedef struct {

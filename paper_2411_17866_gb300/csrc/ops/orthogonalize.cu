@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(256) k_orth_split(const __grid_constant__ Spli
     float2 v = make_float2(0.f, 0.f);
     if (threadIdx.x < p.blocks) v = in.partial[b * kUpdateBlocks + threadIdx.x];
     v = cta_sum(v, sums);
-    const float factor = to_unit(v, p.eps);
+    const Unit unit = to_unit(v, p.eps);
     const uint32_t lane = threadIdx.x % 32, per_row = (in.cols + 255) / 256;
     for (uint32_t t = blockIdx.x * 8 + threadIdx.x / 32; t < in.rows * per_row; t += gridDim.x * 8) {
         const uint32_t r = t / per_row, c = t % per_row * 256 + lane * 8;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(256) k_orth_split(const __grid_constant__ Spli
         if (p.out) {
             for (int k = 0; k < 8; ++k) {
                 if (c + k >= in.cols) break;
-                const float y = x[k] * factor * p.scale;
+                const float y = unit(x[k]) * p.scale;
                 const int64_t at = int64_t(b) * p.os.batch + int64_t(r) * p.os.row + int64_t(c + k) * p.os.col;
                 if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(y);
                 else static_cast<float*>(p.out)[at] = y;
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(256) k_orth_split(const __grid_constant__ Spli
             continue;
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] *= factor * kScale;
+        for (int k = 0; k < 8; ++k) x[k] = unit(x[k]) * kScale;
         const uint64_t at = (b * in.rows + r) * uint64_t(in.ld) + c;
         const uint4 hi = pack8<__half>(x);
         *reinterpret_cast<uint4*>(p.hi + at) = hi;

@@ -8,8 +8,9 @@ namespace ops {
 namespace {
 
 constexpr float kScale = 4096.f;        // of X, A and B as f16
-constexpr float kBig = 0x1p60f;         // squares of larger values are summed apart, scaled by kDown
-constexpr float kDown = 0x1p-64f;
+// Squares are summed of values times kUp, and apart of those above kBig times kDown: both stay below 2^43, so that 2^40
+// squares (the most a matrix has) do not overflow, and down to 2^-84 a value's square is a normal number.
+constexpr float kBig = 0x1p22f, kUp = 0x1p21f, kDown = 0x1p-85f;
 constexpr uint32_t kUpdateBlocks = 256; // most CTAs per matrix of the update kernel, each with a partial sum
 
 struct Strides {
@@ -20,7 +21,7 @@ struct UpdateArgs {
     const void* g;
     float* momentum;
     float* u;                 // [count][rows][ld] f32, of the strided form
-    float2* partial;          // [count][kUpdateBlocks]: sum of squares, of the large values (scaled)
+    float2* partial;          // [count][kUpdateBlocks]: sums of squares, see kBig
     uint32_t *status, *barrier;   // set to zero
     Strides gs, ms;
     uint32_t rows, cols, ld;
@@ -31,16 +32,24 @@ struct UpdateArgs {
 
 __device__ __forceinline__ void add_square(float v, float2& sum) {
     const bool big = fabsf(v) > kBig;
-    const float t = big ? v * kDown : v;
+    const float t = v * (big ? kDown : kUp);
     if (big) sum.y = fmaf(t, t, sum.y);
     else sum.x = fmaf(t, t, sum.x);
 }
 
-// The factor that takes u to X_0, from the sums of its squares.  A NaN among them stays NaN.
-__device__ __forceinline__ float to_unit(float2 sum, float eps) {
-    const float norm = sum.y > 0.f ? sqrtf(fmaf(sum.x * kDown, kDown, sum.y)) : sqrtf(sum.x);  // scaled by kDown with large values
-    const float up = sum.y > 0.f ? kDown : 1.f;
-    return up / (norm < eps * up ? eps * up : norm);
+// What takes u to X_0: u * by * factor.  (Two factors: the norm of large values, and its inverse, may be outside f32's range.)
+struct Unit {
+    float by, factor;
+    __device__ __forceinline__ float operator()(float u) const { return u * by * factor; }
+};
+
+// From the sums of u's squares.  A NaN among them stays NaN.
+__device__ __forceinline__ Unit to_unit(float2 sum, float eps) {
+    constexpr float kApart = kDown / kUp;
+    const bool big = sum.y > 0.f;
+    const float norm = big ? sqrtf(fmaf(sum.x * kApart, kApart, sum.y)) : sqrtf(sum.x) * (1.f / kUp);   // times `by`
+    const float by = big ? kDown : 1.f, least = fmaxf(eps * by, 0x1p-126f);
+    return Unit{by, 1.f / (norm < least ? least : norm)};
 }
 
 // Sums `v` over the CTA (256 threads) in a fixed order; the result is in every thread.

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
             sum.y += ld_cluster(at + 4);
         }
     }
-    const float factor = to_unit(sum, p.eps);
+    const Unit unit = to_unit(sum, p.eps);
     // u again, from g and the new momentum (each thread its own)
     walk(down, [&](const uint32_t (&r)[kBatch], const uint32_t (&c)[kBatch], const bool (&used)[kBatch]) {
         float u[kBatch], mv[kBatch];
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
             if (!used[k]) continue;
             if (mo) u[k] = in.nesterov ? fmaf(in.mu, mv[k], u[k]) : mv[k];
             __half hi, lo;
-            split(u[k] * factor * kScale, hi, lo);
+            split(unit(u[k]) * kScale, hi, lo);
             const uint32_t at = small_place(r[k], c[k]);
             sts16(x_hi + at, __half_as_ushort(hi));
             sts16(x_lo + at, __half_as_ushort(lo));

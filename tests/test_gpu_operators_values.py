@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2411_17866_gb300 import dsm  # noqa: E402
-from test_gpu_operators import ce64, check, problem  # noqa: E402
+from test_gpu_operators import ce64, check, orth64, problem, rel  # noqa: E402
 
 BF16, F32 = torch.bfloat16, torch.float32
 
@@ -195,3 +195,42 @@ def test_gradients_where_all_rows_share_a_direction_by_pieces_and_parts():
     flat = torch.empty(1 + w.numel(), dtype=BF16, device="cuda")
     flat[1:] = w.reshape(-1)
     check(h, flat[1:].view_as(w), y, a)
+
+
+# ---- orthogonalize: sizes near the ends of the formats' range ---------------------------------------------------------
+
+ORTH_TOL = {BF16: 5e-3, F32: 1e-5}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1024, 1024), (90, 200), (600, 60)])
+@pytest.mark.parametrize("size", [1e-24, 1e-16, 1e6, 1e9, 1e16, 1e17, 1e18, 1e19, 1e25, 1e37])
+def test_orthogonalize_of_any_size(size, rows, cols, dtype):
+    """Squares and their sum, and the norm itself, may lie beyond f32's range."""
+    g = (torch.randn(rows, cols, device="cuda").double() * size).to(dtype)
+    assert rel(dsm.orthogonalize(g, eps=1e-30), orth64(g, eps=1e-30)) < ORTH_TOL[dtype]
+    # no steps: one rounding of the result, and the norm's (sums of 10^6 squares in a few levels: 1e-6)
+    assert rel(dsm.orthogonalize(g, 0, eps=1e-30), orth64(g, 0, eps=1e-30)) < (2.0 ** -8 if dtype == BF16 else 2e-6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(300, 400), (100, 700)])
+def test_orthogonalize_of_mixed_sizes(rows, cols, dtype):
+    """Entries on both sides of where squares are summed apart, and some far above the others; with a momentum."""
+    g = torch.randn(2, rows, cols, device="cuda")
+    g[0, ::2] *= 2.0 ** 22
+    g[1, :, ::3] *= 2.0 ** 23
+    g[0, 0, :7] *= 2.0 ** 10
+    g = g.to(dtype)
+    m = torch.randn(2, rows, cols, device="cuda") * 2.0 ** 20
+    want_m = float(torch.tensor(0.95)) * m.double() + g.double()
+    want = orth64(g.double() + float(torch.tensor(0.95)) * want_m)
+    assert rel(dsm.orthogonalize(g, momentum=m), want) < ORTH_TOL[dtype]
+    assert rel(m, want_m) < 2.0 ** -22
+
+
+def test_orthogonalize_zero_with_a_tiny_eps():
+    for shape in ((200, 300), (60, 60)):
+        g = torch.zeros(shape, device="cuda")
+        for eps in (1e-7, 1e-30, 1e-38, 1e-44):
+            assert bool((dsm.orthogonalize(g, eps=eps) == 0).all()) and bool((dsm.orthogonalize(g, 0, eps=eps) == 0).all())
