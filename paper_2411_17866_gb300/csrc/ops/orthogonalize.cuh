@@ -43,13 +43,14 @@ struct Unit {
     __device__ __forceinline__ float operator()(float u) const { return u * by * factor; }
 };
 
-// From the sums of u's squares.  A NaN among them stays NaN.
+// From the sums of u's squares.  A NaN among them stays NaN, and an infinity (which no finite values add up to) becomes one:
+// its inverse would be 0 and all finite values of the matrix with it.
 __device__ __forceinline__ Unit to_unit(float2 sum, float eps) {
     constexpr float kApart = kDown / kUp;
     const bool big = sum.y > 0.f;
     const float norm = big ? sqrtf(fmaf(sum.x * kApart, kApart, sum.y)) : sqrtf(sum.x) * (1.f / kUp);   // times `by`
     const float by = big ? kDown : 1.f, least = fmaxf(eps * by, 0x1p-126f);
-    return Unit{by, 1.f / (norm < least ? least : norm)};
+    return Unit{by, norm == INFINITY ? NAN : 1.f / (norm < least ? least : norm)};
 }
 
 // Sums `v` over the CTA (256 threads) in a fixed order; the result is in every thread.

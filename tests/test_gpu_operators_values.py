@@ -234,3 +234,16 @@ def test_orthogonalize_zero_with_a_tiny_eps():
         g = torch.zeros(shape, device="cuda")
         for eps in (1e-7, 1e-30, 1e-38, 1e-44):
             assert bool((dsm.orthogonalize(g, eps=eps) == 0).all()) and bool((dsm.orthogonalize(g, 0, eps=eps) == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("shape", [(3, 130, 200), (3, 40, 90)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_orthogonalize_makes_a_matrix_that_is_not_finite_nan(bad, shape, steps, dtype):
+    g = torch.randn(shape, device="cuda").to(dtype)
+    g[1, 5, 7] = bad
+    got = dsm.orthogonalize(g, steps)
+    assert bool(got[1].isnan().all())
+    for i in (0, 2):
+        assert rel(got[i], orth64(g[i], steps)) < ORTH_TOL[dtype]
