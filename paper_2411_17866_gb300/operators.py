@@ -266,7 +266,8 @@ def linear_cross_entropy_grad(h, weight, targets, lse, grad_loss, *, ignore_inde
 
 
 def linear_cross_entropy_loss(h, weight, targets, *, ignore_index=-100, out_weight=None):
-    """The mean loss over the tokens that are not ignored (0 if all are), differentiable in h and weight.
+    """The mean loss over the tokens that are not ignored (0 if all are), differentiable in h and weight, once: second
+    derivatives raise an error.
 
     ``out_weight``: where the gradient of ``weight`` is written in the backward pass (its slice of a worker's gradient
     buffer, say); autograd returns that tensor as the gradient."""
@@ -281,6 +282,18 @@ def _function():
     global _loss_function
     if _loss_function is None:
         _import_torch()
+
+        class Once(torch.autograd.Function):
+            """Gradients as they are, for a backward pass that is itself recorded: differentiating them is an error, not
+            nothing.  (torch's once_differentiable records them only where the incoming gradient requires one.)"""
+
+            @staticmethod
+            def forward(ctx, h, weight, grad, dh, dw):
+                return tuple(None if g is None else g.detach() for g in (dh, dw))
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise RuntimeError("linear_cross_entropy_loss is once_differentiable: it has no second derivatives")
 
         class LinearCrossEntropy(torch.autograd.Function):
             @staticmethod
@@ -298,6 +311,8 @@ def _function():
                 need_h, need_weight = ctx.needs_input_grad[:2]
                 dh, dw = linear_cross_entropy_grad(h, weight, targets, lse, each, ignore_index=ctx.ignore_index,
                                                    out_weight=ctx.out_weight, need_h=need_h, need_weight=need_weight)
+                if torch.is_grad_enabled():
+                    dh, dw = Once.apply(h, weight, grad, dh, dw)
                 return dh, dw, None, None, None
 
         _loss_function = LinearCrossEntropy

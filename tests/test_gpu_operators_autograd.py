@@ -1,0 +1,58 @@
+"""linear_cross_entropy_loss under autograd: what it cannot do it refuses."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2411_17866_gb300 import dsm  # noqa: E402
+from test_gpu_operators import TOL_GRAD, ce64, problem, rel  # noqa: E402
+
+F32 = torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.manual_seed(5)
+
+
+@pytest.fixture
+def leaf():
+    h, w, y, _ = problem(50, 300, 64, F32, 0.2)
+    h.requires_grad_(), w.requires_grad_()
+    kept = max(1, int((y != -100).sum()))
+    want = ce64(h.detach(), w.detach(), y, torch.full((1,), 1 / kept, device="cuda"))
+    return h, w, y, want
+
+
+def test_second_derivatives_are_refused(leaf):
+    h, w, y, want = leaf
+    loss = dsm.linear_cross_entropy_loss(h, w, y)
+    dh, dw = torch.autograd.grad(loss, (h, w), create_graph=True)
+    assert rel(dh.detach(), want[2]) < TOL_GRAD[F32] and rel(dw.detach(), want[3]) < TOL_GRAD[F32]
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dh.square().sum() + dw.square().sum()).backward()
+
+
+def test_a_penalty_on_the_gradient_is_refused_beside_a_loss(leaf):
+    h, w, y, _ = leaf
+    for inputs in ((h,), (w,), (h, w)):
+        loss = dsm.linear_cross_entropy_loss(h, w, y)
+        grads = torch.autograd.grad(loss, inputs, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(loss + sum(g.square().sum() for g in grads), h)
+    # and by the incoming gradient alone
+    s = torch.ones((), device="cuda", requires_grad=True)
+    dh, = torch.autograd.grad(dsm.linear_cross_entropy_loss(h, w, y), h, grad_outputs=s, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(dh.sum(), s)
+
+
+def test_a_recorded_backward_pass_gives_the_same_gradients(leaf):
+    h, w, y, want = leaf
+    out = torch.empty_like(w)
+    dsm.linear_cross_entropy_loss(h, w, y, out_weight=out).backward(create_graph=True)
+    assert rel(h.grad.detach(), want[2]) < TOL_GRAD[F32] and rel(w.grad.detach(), want[3]) < TOL_GRAD[F32]
+    assert torch.equal(out, w.grad.detach())
+    h.grad = w.grad = None   # (a recorded gradient holds on to its graph)
