@@ -270,8 +270,39 @@ def linear_cross_entropy_loss(h, weight, targets, *, ignore_index=-100, out_weig
     derivatives raise an error.
 
     ``out_weight``: where the gradient of ``weight`` is written in the backward pass (its slice of a worker's gradient
-    buffer, say); autograd returns that tensor as the gradient."""
+    buffer, say); autograd returns that tensor as the gradient.  ``weight.grad`` must not lie in the same memory, nor two
+    losses of one backward pass write to it: autograd would add the tensor to itself (ValueError).  A gradient that
+    autograd is to collect in ``weight.grad``, whatever its memory, needs no ``out_weight``."""
     return _function().apply(h, weight, targets, ignore_index, out_weight)
+
+
+def _span(t):
+    """The addresses from a tensor's first element to behind its last."""
+    start = t.data_ptr()
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return (start, start + (last + 1) * t.element_size()) if t.numel() else (start, start)
+
+
+def _overlap(a, b):
+    return a[0] < b[1] and b[0] < a[1]
+
+
+_pass, _pass_spans = None, []   # the last backward pass, and where it has written an out_weight
+
+
+def _check_out_weight(weight, out):
+    """Refuses an out_weight that autograd would add to itself."""
+    global _pass, _pass_spans
+    span = _span(out)
+    if weight.is_leaf and weight.grad is not None and _overlap(_span(weight.grad), span):
+        raise ValueError("weight.grad shares memory with out_weight, and autograd would add the gradient to itself: set "
+                         "weight.grad to None before the backward pass, or leave out_weight out")
+    current = torch._C._current_graph_task_id()
+    if current != _pass:
+        _pass, _pass_spans = current, []
+    if any(_overlap(span, other) for other in _pass_spans):
+        raise ValueError("two losses of one backward pass write to the same out_weight")
+    _pass_spans.append(span)
 
 
 _loss_function = None
@@ -309,6 +340,8 @@ def _function():
                 h, weight, targets, lse, kept = ctx.saved_tensors
                 each = (grad.to(torch.float32) / kept).reshape(1)
                 need_h, need_weight = ctx.needs_input_grad[:2]
+                if need_weight and ctx.out_weight is not None:
+                    _check_out_weight(weight, ctx.out_weight)
                 dh, dw = linear_cross_entropy_grad(h, weight, targets, lse, each, ignore_index=ctx.ignore_index,
                                                    out_weight=ctx.out_weight, need_h=need_h, need_weight=need_weight)
                 if torch.is_grad_enabled():

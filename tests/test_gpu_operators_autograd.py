@@ -56,3 +56,55 @@ def test_a_recorded_backward_pass_gives_the_same_gradients(leaf):
     assert rel(h.grad.detach(), want[2]) < TOL_GRAD[F32] and rel(w.grad.detach(), want[3]) < TOL_GRAD[F32]
     assert torch.equal(out, w.grad.detach())
     h.grad = w.grad = None   # (a recorded gradient holds on to its graph)
+
+
+def test_out_weight_that_is_the_weights_own_gradient_is_refused(leaf):
+    """Autograd would add the tensor to itself: twice the gradient."""
+    h, w, y, want = leaf
+    flat = torch.zeros(w.numel() + 64, device="cuda")
+    buf = flat[64:].view_as(w)
+    w.grad = buf
+    for out in (buf, flat[64:].view_as(w), flat[32:32 + w.numel()].view_as(w)):
+        with pytest.raises(ValueError, match="weight.grad"):
+            dsm.linear_cross_entropy_loss(h, w, y, out_weight=out).backward()
+    assert bool((flat == 0).all())                          # nothing was written
+    # another part of the same storage, no gradient yet, and no out_weight at all are fine
+    both = torch.zeros(2, *w.shape, device="cuda")
+    w.grad = both[0]
+    dsm.linear_cross_entropy_loss(h, w, y, out_weight=both[1]).backward()
+    assert torch.equal(both[0], both[1]) and rel(both[0], want[3]) < TOL_GRAD[F32]
+    w.grad = None
+    dsm.linear_cross_entropy_loss(h, w, y, out_weight=buf).backward()
+    assert torch.equal(w.grad, buf) and rel(buf, want[3]) < TOL_GRAD[F32]
+    w.grad = buf.zero_()
+    dsm.linear_cross_entropy_loss(h, w, y).backward()
+    assert w.grad is buf and rel(buf, want[3]) < TOL_GRAD[F32]
+
+
+def test_two_losses_of_one_backward_pass_do_not_share_an_out_weight(leaf):
+    h, w, y, want = leaf
+    buf = torch.empty_like(w)
+    two = dsm.linear_cross_entropy_loss(h, w, y, out_weight=buf) + dsm.linear_cross_entropy_loss(2 * h, w, y, out_weight=buf)
+    with pytest.raises(ValueError, match="two losses"):
+        two.backward()
+    # one after the other they may
+    h.grad = w.grad = None
+    first, second = (dsm.linear_cross_entropy_loss(h, w, y, out_weight=buf) for _ in range(2))
+    for loss in (first, second):
+        w.grad = None
+        loss.backward(retain_graph=True)
+        assert rel(buf, want[3]) < TOL_GRAD[F32] and torch.equal(buf, w.grad)
+    w.grad = None
+    first.backward()
+    assert torch.equal(buf, w.grad)
+
+
+def test_a_weight_that_is_no_leaf_and_is_used_twice(leaf):
+    """An embedding used for the lookup as well: both gradients add up, and out_weight holds the head's."""
+    h, w, y, want = leaf
+    buf = torch.empty_like(w)
+    (dsm.linear_cross_entropy_loss(h, w * 1.0, y, out_weight=buf) + (3 * w).sum()).backward()
+    assert rel(w.grad, want[3] + 3) < TOL_GRAD[F32] and rel(buf, want[3]) < TOL_GRAD[F32]
+    w.grad = None
+    (dsm.linear_cross_entropy_loss(h, w, y, out_weight=buf) + (3 * w).sum()).backward()
+    assert rel(w.grad, want[3] + 3) < TOL_GRAD[F32] and rel(buf, want[3]) < TOL_GRAD[F32]
