@@ -839,6 +839,13 @@ int check_args(const char* func, const dsm_linear_ce* p) {
     return DSM_OK;
 }
 
+// The vectors of f32, one value per token.
+int check_vectors(const char* func, const dsm_linear_ce& p, const void* a, const void* b, const char* names) {
+    if (p.tokens && (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % 4)
+        return fail(func, DSM_EALIGN, "%s must be aligned to their elements", names);
+    return DSM_OK;
+}
+
 template <typename T>
 cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss, uint64_t grad_stride, bool for_w,
                    uint32_t* status, cudaStream_t s) {
@@ -1113,6 +1120,7 @@ extern "C" int dsm_linear_cross_entropy(const dsm_linear_ce* p, float* loss, flo
                                         size_t workspace_bytes, dsm_stream_t stream) {
     const char* func = "dsm_linear_cross_entropy";
     if (int rc = check_args(func, p); rc != DSM_OK) return rc;
+    if (int rc = check_vectors(func, *p, loss, lse, "loss and lse")) return rc;
     int dev = 0, sms = 0;
     if (int rc = device_of_call(func, &dev, &sms)) return rc;
     const Plan r = make_plan(*p, false, workspace);
@@ -1152,6 +1160,7 @@ extern "C" int dsm_linear_cross_entropy_grad(const dsm_linear_ce* p, const float
                                              dsm_stream_t stream) {
     const char* func = "dsm_linear_cross_entropy_grad";
     if (int rc = check_args(func, p); rc != DSM_OK) return rc;
+    if (int rc = check_vectors(func, *p, lse, grad_loss, "lse and grad_loss")) return rc;
     int dev = 0, sms = 0;
     if (int rc = device_of_call(func, &dev, &sms)) return rc;
     const Plan r = make_plan(*p, true, workspace);
