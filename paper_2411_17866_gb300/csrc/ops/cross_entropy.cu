@@ -161,6 +161,7 @@ struct GatherArgs {
     int* row;                 // per token: its row, or -1
     long long* rest;          // null, or per kept row: set to zero
     uint32_t* status;
+    uint32_t gave_up;         // injected_timeout()
 };
 
 __device__ __forceinline__ int64_t target_of(const GatherArgs& p, uint32_t t) {
@@ -197,7 +198,7 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         *p.count = c.y;
-        *p.status = 0;
+        *p.status = p.gave_up;
         if (p.splits) *p.splits = p.sum.parts(c.y);
     }
     uint32_t before = c.x;
@@ -869,6 +870,7 @@ cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss
     a.token = r.token;
     a.row = r.row;
     a.status = status;
+    a.gave_up = injected_timeout();
     const bool scaled = r.pair && grad_loss;
     if (scaled) {
         a.grad_loss = grad_loss;

@@ -4,6 +4,7 @@
 #include <atomic>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 
 #include <cuda.h>
@@ -36,6 +37,12 @@ inline int fail(const char* func, int code, const char* fmt, ...) {
 inline int cuda_fail(const char* func, cudaError_t e, const char* what) {
     cudaGetLastError();  // reported here: it must not be found again by a later call's check
     return fail(func, DSM_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// DSM_INJECT_OPERATOR_TIMEOUT=1: kernels that wait act as if a wait of theirs had run out (fault injection for tests).
+inline bool injected_timeout() {
+    const char* inject = std::getenv("DSM_INJECT_OPERATOR_TIMEOUT");
+    return inject && inject[0] == '1';
 }
 
 // Hands out consecutive 256-byte aligned pieces; with a null base it only adds up the size.

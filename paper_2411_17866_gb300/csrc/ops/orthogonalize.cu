@@ -596,6 +596,7 @@ struct StepsArgs {
     EpiApply<std::conditional_t<PAIR, float, __nv_bfloat16>> to_apply[2];
     Schedule half_n, half_m, all;                // of the three products
     uint32_t* barrier;
+    uint32_t gave_up;                            // injected_timeout()
     uint32_t steps, pairs;                       // X of the first `pairs` steps are pairs (of all, for a result in 32 bits)
     Out last;                                    // where the last step's result goes
     CUtensorMap out;
@@ -607,6 +608,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_orth_steps(const __grid_cons
     extern __shared__ uint8_t raw[];
     Pipe<S> p;
     p.open(raw);
+    p.ok = !a.gave_up;
     wait_previous();
     using Sched = Scheduler<S>;
     const Sched half_n(a.half_n), half_m(a.half_m), all(a.all);
@@ -721,6 +723,7 @@ int steps(const dsm_orthogonalize_args& p, const Plan& r, uint32_t* status, int 
     a.all.tiles_m = ceil_div(r.rows, kBM);
     a.all.tiles_n = ceil_div(r.cols, BN);
     a.barrier = r.barrier;
+    a.gave_up = injected_timeout();
     a.steps = p.steps;
     a.pairs = r.pairs;
     for (uint32_t i = 0; i < 3 * p.steps; ++i) a.coefficients[i] = p.coefficients[i];

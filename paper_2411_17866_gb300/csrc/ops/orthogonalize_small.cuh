@@ -21,6 +21,7 @@ struct SmallArgs {
     float eps, scale;
     uint32_t slab;               // columns of a CTA, a multiple of 64
     uint32_t steps;
+    uint32_t gave_up;            // injected_timeout()
     float coefficients[3 * DSM_ORTHOGONALIZE_MAX_STEPS];
 };
 
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
     const uint32_t m = in.rows, n = in.cols, c0 = rank * p.slab;
     const uint32_t mine = c0 >= n ? 0 : n - c0 < p.slab ? n - c0 : p.slab, tiles = p.slab / 64;
     const int64_t b = blockIdx.x / cluster;
-    bool ok = true;
+    bool ok = !p.gave_up;        // of the warp
 
     if (tid == 0) {
         mbar_init(bar, 1);
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
     uint32_t phase = 0;
     // A product: D (128 x columns) over `blocks` of 16 k; the operands' places and steps per 16 k as functions.
     auto multiply = [&](uint32_t d, uint32_t idesc, uint32_t blocks, auto a_at, auto b_at, uint32_t a_plane, uint32_t b_plane, uint32_t lbo_b) {
-        if (warp == 0) {
+        if (warp == 0 && ok) {   // (after a wait that ran out nothing more is multiplied)
             if (elect_one()) {
                 constexpr int kTerms = kPair ? 3 : 1;
                 for (uint32_t i = 0; i < blocks; ++i)
@@ -204,8 +205,8 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
             }
             __syncwarp();
         }
-        if (ok) ok = mbar_wait(bar, phase);   // (who gave up goes on, so that the barriers meet, but waits no more)
-        phase ^= 1;
+        if (ok) ok = warp_wait(bar, phase);   // (who gave up goes on, so that the barriers meet, but waits no more)
+        if (ok) phase ^= 1;
         __syncwarp();
         tc_fence_after();
     };
@@ -349,7 +350,10 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
             out[r[k] * p.os.row + (c0 + c[k]) * p.os.col] = y;
         }
     });
-    if (!ok) *in.status = 1;
+    if (!ok) {
+        *in.status = 1;
+        if (warp == 0) warp_wait(bar, phase);   // what it has issued may still be under way: shared and tensor memory are in use
+    }
     tc_fence_before();
     if (cluster > 1) cluster_sync();   // nobody reads this CTA's shared memory any more
     else __syncthreads();
@@ -387,6 +391,7 @@ cudaError_t launch_small(const dsm_orthogonalize_args& p, SmallArgs& a, int clus
     a.scale = p.scale;
     a.slab = static_cast<uint32_t>(round_up(ceil_div(a.in.cols, cluster), 64));
     a.steps = p.steps;
+    a.gave_up = injected_timeout();
     for (uint32_t i = 0; i < 3 * p.steps; ++i) a.coefficients[i] = p.coefficients[i];
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem<T>());
     if (err == cudaSuccess && cluster > 8) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
