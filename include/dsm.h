@@ -476,8 +476,9 @@ int dsm_global_step_noalloc(const dsm_layout* layout, uint32_t n, const dsm_hpar
  *
  * The operators' matrix products wait on barriers on the GPU.  A wait that
  * runs out (2 s; it means a defect or a stopped GPU) ends its kernel and is
- * recorded in the workspace: dsm_operator_status() tells, and the outputs of
- * that call are then undefined.
+ * recorded in the workspace: dsm_operator_status() tells, and whatever of the
+ * outputs of that call is not the operator's result is then NaN (all of loss,
+ * lse, dh and dW).  A momentum is updated all the same.
  *
  * Results are deterministic: the same inputs, laid out the same, give the
  * same bits. */

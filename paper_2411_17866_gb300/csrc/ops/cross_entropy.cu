@@ -401,6 +401,7 @@ struct JoinArgs {
     const float* target_logit;
     float *loss, *lse;
     uint32_t tokens, groups, rows;
+    const uint32_t* status;
 };
 
 // Joins the partial results of ROWS rows, in a fixed order: a thread to a row and every kParts'th group of columns.  8 rows to
@@ -422,7 +423,8 @@ __global__ void __launch_bounds__(1024) k_ce_join(const __grid_constant__ JoinAr
         for (uint32_t i = part; i < p.groups; i += kParts) v = joined(v, p.partial[uint64_t(i) * p.rows + r]);
     }
     parts[part][own] = v;
-    if (part == 0 && r < p.tokens && p.row[r] < 0) p.loss[r] = p.lse[r] = 0.f;
+    const bool failed = *p.status != 0;   // partial results are missing: all is NaN
+    if (part == 0 && r < p.tokens && (failed || p.row[r] < 0)) p.loss[r] = p.lse[r] = failed ? NAN : 0.f;
     __syncthreads();
     // a warp to a row: its parts
     if (warp >= ROWS) return;
@@ -431,7 +433,7 @@ __global__ void __launch_bounds__(1024) k_ce_join(const __grid_constant__ JoinAr
     for (uint32_t i = lane + 32; i < kParts; i += 32) v = joined(v, parts[i][warp]);
     for (int o = 16; o; o >>= 1)
         v = joined(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
-    if (lane || r >= count) return;
+    if (lane || r >= count || failed) return;
     const bool known = p.target[r] >= 0;   // else a target outside the vocabulary
     const float lse = known ? log_sum(v) : NAN;
     p.lse[p.token[r]] = lse;
@@ -636,6 +638,10 @@ struct ScatterArgs {
     uint64_t stride, w_stride;
     uint32_t ld, tokens, width;
     void* dh;
+    const uint32_t* status;
+    void* dw;                 // null, or to be made NaN with dh after a wait that ran out
+    uint64_t dw_stride;
+    uint32_t vocab;
 };
 
 // dh from the sums, back in the order of the tokens; zeros for the ignored ones.  16-bit: without what the rounding of G has left
@@ -645,6 +651,13 @@ template <typename T, bool MANY>
 __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ ScatterArgs p) {
     __shared__ float4 parts[8][32];
     wait_previous();
+    if (*p.status) {
+        const uint64_t me = uint64_t(blockIdx.x) * 256 + threadIdx.x, all = uint64_t(gridDim.x) * 256;
+        if (p.dh) fill_nan(static_cast<T*>(p.dh), 1, p.tokens, p.width, 0, p.stride, 1, me, all);
+        if (p.dw) fill_nan(static_cast<T*>(p.dw), 1, p.vocab, p.width, 0, p.dw_stride, 1, me, all);
+        return;
+    }
+    if (!p.dh) return;
     const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, per_row = (p.width + 127) / 128;
     const bool vec = p.stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.dh) % (4 * sizeof(T)) == 0;
     const uint32_t splits = *p.splits;
@@ -1093,12 +1106,13 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
                                                                   uint64_t(w.tiles_m) * w.tiles_n, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the gradient of W");
     }
-    if (!p.tokens || !dh) return DSM_OK;
+    // (without dh only for the status)
     ScatterArgs sc{r.row,  r.target,  r.sum,      grad_loss, r.scales, grad_stride, r.count, r.count + 1,
-                   r.rest, p.w,       dh_stride,  p.w_stride, r.ld_sum, p.tokens,   p.width, dh};
+                   r.rest, p.w,       dh_stride,  p.w_stride, r.ld_sum, p.tokens,   p.width, dh,
+                   status, dw,        dw_stride,  p.vocab};
     const bool many = r.splits > 8;
-    const uint64_t parts = uint64_t(p.tokens) * ceil_div(p.width, 128), blocks = many ? parts : ceil_div(parts, 8);
-    const dim3 grid(static_cast<uint32_t>(blocks < 4096 ? blocks : 4096));
+    const uint64_t parts = dh ? uint64_t(p.tokens) * ceil_div(p.width, 128) : 0, blocks = many ? parts : ceil_div(parts, 8);
+    const dim3 grid(static_cast<uint32_t>(blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096));
     err = many ? launch_grid(k_ce_scatter<T, true>, grid, 256, 0, s, sc) : launch_grid(k_ce_scatter<T, false>, grid, 256, 0, s, sc);
     return err == cudaSuccess ? DSM_OK : cuda_fail(func, err, "launch the scatter of dh");
 }
@@ -1150,7 +1164,7 @@ extern "C" int dsm_linear_cross_entropy(const dsm_linear_ce* p, float* loss, flo
                     : r.tile_v == 128       ? forward<false, 1, 128>
                                             : forward<false, 1>;
     if (int rc = go(func, *p, r, status, sms, s)) return rc;
-    JoinArgs j{r.count, r.row, r.target, r.token, r.partial, r.target_logit, loss, lse, p->tokens, r.groups, r.rows};
+    JoinArgs j{r.count, r.row, r.target, r.token, r.partial, r.target_logit, loss, lse, p->tokens, r.groups, r.rows, status};
     const auto join = join_rows(p->tokens) == 8 ? k_ce_join<8> : k_ce_join<32>;
     err = launch_grid(join, dim3(ceil_div(p->tokens, join_rows(p->tokens))), 1024, 0, s, j);
     return err == cudaSuccess ? DSM_OK : cuda_fail(func, err, "launch the join");

@@ -58,6 +58,17 @@ struct Carver {
     }
 };
 
+// NaN in all places of `count` matrices of rows x cols, by the threads `first`, first + step, ...: what becomes of results after
+// a wait that ran out.
+template <typename T>
+__device__ inline void fill_nan(T* to, uint64_t count, uint64_t rows, uint64_t cols, int64_t matrix, int64_t row, int64_t col,
+                                uint64_t first, uint64_t step) {
+    for (uint64_t i = first; i < count * rows * cols; i += step) {
+        const uint64_t r = i / cols;
+        to[int64_t(r / rows) * matrix + int64_t(r % rows) * row + int64_t(i % cols) * col] = round_to<T>(NAN);
+    }
+}
+
 int check_device(const char* func, const void* p, const char* name, int dev);
 int device_of_call(const char* func, int* dev, int* sms);
 

@@ -659,6 +659,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_orth_steps(const __grid_cons
                                      k < a.pairs, k + 1 < a.pairs});
     }
     p.close(a.all.status);
+    // A CTA that gave up has left tiles unwritten, which no other writes.
+    if (__syncthreads_or(!p.ok)) {
+        const auto& e = a.to_apply[0];
+        fill_nan(e.out, a.all.batches, e.rows, e.cols, e.os.batch, e.os.row, e.os.col, threadIdx.x, S::kThreads);
+    }
 }
 
 template <int CG, int BN, bool PAIR, bool TALL>

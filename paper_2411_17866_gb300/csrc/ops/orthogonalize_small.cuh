@@ -355,10 +355,12 @@ __global__ void __launch_bounds__(256, 1) k_orth_small(const __grid_constant__ S
         if (warp == 0) warp_wait(bar, phase);   // what it has issued may still be under way: shared and tensor memory are in use
     }
     tc_fence_before();
+    const bool failed = __syncthreads_or(!ok);
     if (cluster > 1) cluster_sync();   // nobody reads this CTA's shared memory any more
-    else __syncthreads();
     tc_fence_after();
     if (warp == 0) tmem_dealloc<1>(tmem, 512);
+    // after all CTAs' results, which its own may have gone into
+    if (failed) fill_nan(out, 1, m, n, 0, p.os.row, p.os.col, tid, 256);
 }
 
 // Whether a device takes clusters of 16 CTAs of the kernel.

@@ -90,7 +90,8 @@ def _given(workspace, index):
 
 
 def operator_status(workspace, stream=None) -> int:
-    """0, or 1 if a wait of the last operator call on this workspace ran out on the GPU.  Synchronises the stream."""
+    """0, or 1 if a wait of the last operator call on this workspace ran out on the GPU (what it has not computed is then NaN,
+    as it is where no workspace was given).  Synchronises the stream."""
     out = ctypes.c_uint32()
     rc = _d.load_library().dsm_operator_status(workspace.data_ptr(), _d._stream(stream), byref(out))
     _d._check(rc, "dsm_operator_status")
