@@ -540,8 +540,8 @@ int dsm_orthogonalize(const dsm_orthogonalize_args* args, void* workspace, size_
  * Tokens whose target is ignore_index take no part whatever their row of h
  * holds: loss, lse and their row of dh are 0.  A target outside [0, vocab)
  * that is not ignore_index gives loss = lse = NaN, and so NaN gradients.
- * loss, lse and grad_loss are f32; grad_loss_stride is 1, or 0 for one value
- * for all tokens.  lse is what dsm_linear_cross_entropy gave for the same
+ * loss, lse and grad_loss are f32; the values of grad_loss lie
+ * grad_loss_stride elements apart (0: one value for all tokens).  lse is what dsm_linear_cross_entropy gave for the same
  * inputs.  dh and dW have the type dtype and are written whole (not added
  * to); either may be NULL and is then not computed.  tokens = 0 is valid (dW
  * is then 0).

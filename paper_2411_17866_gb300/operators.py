@@ -237,16 +237,16 @@ def linear_cross_entropy_grad(h, weight, targets, lse, grad_loss, *, ignore_inde
                               need_h=True, need_weight=True, workspace=None, stream=None):
     """The gradients (of h, of weight) of sum(grad_loss * loss), from the ``lse`` of ``linear_cross_entropy``.
 
-    ``grad_loss``: one float32 value per token, or a tensor with one for all.  ``out_h`` and ``out_weight`` (rows of
+    ``grad_loss``: one float32 value per token (a vector of any stride, an expanded one too), or a tensor with one for all.  ``out_h`` and ``out_weight`` (rows of
     any stride: a worker's gradient buffer, say) are written whole; new tensors if not given.  A gradient that is not
     needed (``need_h``, ``need_weight``) is not computed, and None is returned for it."""
     index = _on_gpu(h=h, weight=weight, targets=targets, lse=lse, grad_loss=grad_loss, out_h=out_h,
                     out_weight=out_weight)
     a = _ce_args(h, weight, targets, ignore_index)
     _vector(lse, a.tokens, "lse")
-    one = grad_loss.numel() == 1 and grad_loss.dtype == torch.float32
-    if not one:
-        _vector(grad_loss, a.tokens, "grad_loss")
+    if grad_loss.dtype != torch.float32 or (grad_loss.numel() != 1 and grad_loss.shape != (a.tokens,)):
+        raise ValueError("grad_loss must be a float32 vector with one entry per row of h, or one value")
+    grad_stride = 0 if grad_loss.numel() == 1 else grad_loss.stride(0)
 
     def output(needed, given, like, name):
         if not needed:
@@ -261,7 +261,7 @@ def linear_cross_entropy_grad(h, weight, targets, lse, grad_loss, *, ignore_inde
     out_weight, dw, dw_stride = output(need_weight, out_weight, weight, "out_weight")
     if need_weight or (need_h and a.tokens):
         ws = _new(_ce_bytes(a, True), torch.uint8, index, stream) if workspace is None else _given(workspace, index)
-        _call(index, "dsm_linear_cross_entropy_grad", byref(a), lse.data_ptr(), grad_loss.data_ptr(), 0 if one else 1, dh,
+        _call(index, "dsm_linear_cross_entropy_grad", byref(a), lse.data_ptr(), grad_loss.data_ptr(), grad_stride, dh,
               dh_stride, dw, dw_stride, ws.data_ptr(), ws.nbytes, stream=stream)
     return out_h, out_weight
 

@@ -108,3 +108,38 @@ def test_a_weight_that_is_no_leaf_and_is_used_twice(leaf):
     w.grad = None
     (dsm.linear_cross_entropy_loss(h, w, y, out_weight=buf) + (3 * w).sum()).backward()
     assert rel(w.grad, want[3] + 3) < TOL_GRAD[F32] and rel(buf, want[3]) < TOL_GRAD[F32]
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 50])
+def test_grad_loss_of_any_stride(tokens):
+    """An expanded value is what autograd hands to the summands of a sum."""
+    h, w, y, a = problem(tokens, 300, 64, F32)
+    _, lse = dsm.linear_cross_entropy(h, w, y)
+    apart = torch.stack((a, 7 * a), 1)[:, 0]
+    one = a[:1].clone()
+    for given, plain in ((apart, a), (one.expand(tokens), one.repeat(tokens)), (one[0], one.repeat(tokens))):
+        want = dsm.linear_cross_entropy_grad(h, w, y, lse, plain.contiguous())
+        got = dsm.linear_cross_entropy_grad(h, w, y, lse, given)
+        assert all(torch.equal(x, z) for x, z in zip(got, want))
+
+
+def test_a_sum_of_losses_under_a_function_of_the_callers():
+    """The operator as the user's own autograd function has it: backward() of a sum brings an expanded gradient."""
+    h, w, y, _ = problem(50, 300, 64, F32, 0.2)
+
+    class Loss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, h, w):
+            loss, lse = dsm.linear_cross_entropy(h, w, y)
+            ctx.save_for_backward(h, w, lse)
+            return loss
+
+        @staticmethod
+        def backward(ctx, grad):
+            h, w, lse = ctx.saved_tensors
+            return dsm.linear_cross_entropy_grad(h, w, y, lse, grad)
+
+    h.requires_grad_(), w.requires_grad_()
+    Loss.apply(h, w).sum().backward()
+    want = ce64(h.detach(), w.detach(), y, torch.ones(1, device="cuda"))
+    assert rel(h.grad, want[2]) < TOL_GRAD[F32] and rel(w.grad, want[3]) < TOL_GRAD[F32]
