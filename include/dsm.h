@@ -554,9 +554,11 @@ int dsm_orthogonalize(const dsm_orthogonalize_args* args, void* workspace, size_
  * what W's rows have in common drops out of dh in spite of that.
  * Nothing of the size tokens x vocab is kept: the loss' workspace holds 8
  * bytes for a token and 128 rows of W (64 with 32-bit operands), the
- * gradient's a piece of the vocabulary for all tokens, at most 256 MB (512
- * with 32-bit operands) or 256 rows of W.  Where W is f32 or its rows do not
- * start on 16-byte boundaries the workspace holds a copy of it as well. */
+ * gradient's a piece of the vocabulary for all tokens, at most 256 MiB (512
+ * with 32-bit operands) or 256 rows of W, and f32 sums of dh's size (several
+ * times that for few tokens).  Both hold a copy of h, with 32-bit operands the
+ * gradient's two; where W is f32 or its rows do not start on 16-byte
+ * boundaries there is a copy of it as well. */
 typedef struct {
     const void* h;
     const void* w;

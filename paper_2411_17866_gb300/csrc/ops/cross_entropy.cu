@@ -816,8 +816,10 @@ Plan make_plan(const dsm_linear_ce& p, bool grad, void* workspace) {
         r.partial = c.take<float2>(uint64_t(r.groups) * r.rows);
         r.target_logit = c.take<float>(r.rows);
     } else {
-        const uint64_t all = round_up(p.vocab, kPieceUnit), most = kPieceBytes / ((r.pair ? 4 : 2) * uint64_t(r.rows));
-        r.pieces = most >= all ? 1 : ceil_div(all, most < kPieceUnit ? kPieceUnit : most);
+        // a whole number of units, so that rounding up to one does not pass the bound (but one at least)
+        const uint64_t all = round_up(p.vocab, kPieceUnit), fit = kPieceBytes / ((r.pair ? 4 : 2) * uint64_t(r.rows));
+        const uint64_t most = fit < kPieceUnit ? kPieceUnit : fit / kPieceUnit * kPieceUnit;
+        r.pieces = most >= all ? 1 : ceil_div(all, most);
         r.piece = static_cast<uint32_t>(round_up(ceil_div(all, r.pieces), kPieceUnit));
         r.pieces = ceil_div(p.vocab, r.piece);
         if (!r.pair) r.rest = c.take<long long>(r.rows);
