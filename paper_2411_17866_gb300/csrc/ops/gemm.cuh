@@ -55,9 +55,10 @@ struct Shape {
     static constexpr int CG = CG_, BN = BN_, TERMS = TERMS_;
     static constexpr bool CHUNKED = CHUNK > 0, BF16 = BF16_;
     static constexpr int kPair = TERMS == 3 ? 2 : 1;
-    static constexpr uint32_t kChunk = CHUNK / kBlockK;      // stages between two additions to the register sums
     // Blocks of 64 k per stage: two where issuing takes longer than multiplying (waits are per stage).
     static constexpr uint32_t kSub = CG == 1 && TERMS == 1 && BN <= 128 ? 2 : 1;
+    static constexpr uint32_t kChunk = CHUNK / (kBlockK * kSub);   // stages between two additions to the register sums
+    static_assert(kChunk * kBlockK * kSub == CHUNK, "whole stages");
     static constexpr int kEpiWarps = BN == 64 ? 4 : 8;
     static constexpr int kFirstEpi = 3;                                             // warps before the epilogue's
     static constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);

@@ -247,3 +247,20 @@ def test_orthogonalize_makes_a_matrix_that_is_not_finite_nan(bad, shape, steps, 
     assert bool(got[1].isnan().all())
     for i in (0, 2):
         assert rel(got[i], orth64(g[i], steps)) < ORTH_TOL[dtype]
+
+
+# ---- what the accumulators cut off ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [60, 128, 200])
+@pytest.mark.parametrize("vocab", [700, 50257])
+@pytest.mark.parametrize("width", [512, 768, 1024, 1600, 2048])
+def test_long_sums_of_one_sign(width, vocab, tokens):
+    """Sums leave the accumulators every 512 k.  Until then each of 32 additions cuts off half of the last bit on average
+    (2^-24 of the sum so far, which is half of the whole on average): the mean error of logits that are sums of one sign is
+    below 16 * 2^-24, and it does not grow with the width."""
+    h = torch.rand(tokens, width, device="cuda").to(BF16)
+    w = (torch.rand(vocab, width, device="cuda") * (160 / width)).to(BF16)
+    y = torch.randint(0, vocab, (tokens,), device="cuda")
+    _, lse = dsm.linear_cross_entropy(h, w, y)
+    want = torch.logsumexp(h.double() @ w.double().T, 1)
+    assert abs(float(((lse.double() - want) / want).mean())) < 16 * 2.0 ** -24
