@@ -547,10 +547,10 @@ int dsm_orthogonalize(const dsm_orthogonalize_args* args, void* workspace, size_
  * is then 0).
  * Accuracy of f32 results, each relative to the sum of the sizes of what it
  * adds up: loss and lse 2^-20 of a logit's products, a row of dh or dW 2^-21
- * of its own products besides what that makes of the probabilities.  G and h
- * keep this down to 2^-17 of the largest value of their token (for dh) or of
- * all tokens (for dW), and 2^-39 of that absolutely; the size of a row of W or
- * h costs no other row anything.  bf16: G and the results are rounded to bf16;
+ * of its own products besides what that makes of the probabilities.  The
+ * probabilities keep this down to 2^-17, a row of W (for dh) to 2^-17 of W's
+ * largest value and grad_loss_t h_t (for dW) to 2^-17 of its largest, and
+ * 2^-39 of that absolutely; no row's size costs another row's gradient more.  bf16: G and the results are rounded to bf16;
  * what W's rows have in common drops out of dh in spite of that.
  * Nothing of the size tokens x vocab is kept: the loss' workspace holds 8
  * bytes for a token and 128 rows of W (64 with 32-bit operands), the

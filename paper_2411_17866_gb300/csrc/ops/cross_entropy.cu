@@ -17,11 +17,11 @@
 // G W - s_t W_y, which puts the rest on the target and with it back to zero.  (All rows of W with a common part that moves
 // the logits to -120: dh was off by 6.5 %, and is by 0.3 %.)  32-bit operands
 // are kept as pairs hi + lo of f16 (22 bits) and multiplied in three terms.  Every row of h and of W is scaled by a power
-// of two of its own so that its largest value lies just below f16's range.  G is kept twice, because the scales of what its
-// products sum over have to be folded into it: for dh = G W with the scales of W's rows and one of its own for every token;
-// for dW = G^T h with one for all, against h scaled by one for all.  So neither a row of W nor a token sets the
-// precision of another's gradient: values of G and of h keep 22 bits down to 2^-17 of the largest, and 2^-39 of that as an
-// absolute error below.  (G once, with both scales folded in: rows of W or h that are zero, or much smaller than the
+// of two of its own so that its largest value lies just below f16's range.  G is kept without
+// grad_loss, p_tv - [v = y_t], and twice: for dh with the scales of W's rows, which its product sums over (grad_loss_t comes
+// last), and for dW as it is, against grad_loss_t h_t under one scale for all.  So neither a row of W nor a token sets the
+// precision of another's gradient: G and grad_loss_t h_t keep 22 bits down to 2^-17 of their largest value, and 2^-39 of
+// that as an absolute error below.  (G once, with both scales folded in: rows of W or h that are zero, or much smaller than the
 // others, cost dh and dW up to 31 bits.)  Statistics, lse and the sums for dh are in f32.
 #include <type_traits>
 
@@ -46,9 +46,13 @@ __device__ __forceinline__ float power(int e) { return __uint_as_float(static_ca
 // v 2^e for e in [-252, 254]
 __device__ __forceinline__ float times_power(float v, int e) { return v * power(e / 2) * power(e - e / 2); }
 
-// What 32-bit operands are scaled by: exponents of the largest |grad_loss|, of the largest inverse scales of h and of W.
+// The same of grad_loss, whose inverse has to be normal.
+__device__ __forceinline__ int grad_exponent(float a) { return min(exponent(a), 126); }
+
+// What 32-bit operands are scaled by: the largest exponents of grad_loss_t times the inverse scale of h_t, and of the inverse
+// scales of W.
 struct Scales {
-    int grad, h, w;
+    int h, w;
 };
 
 // 16-bit operand planes of rows of h or W: bf16, or f16 pairs with the inverse of every row's scale.
@@ -150,9 +154,9 @@ struct GatherArgs {
     int64_t ignore;
     uint32_t tokens, vocab, width, per_block, blocks;
     Planes to;
-    const float* grad_loss;   // null, or for `most`: per CTA the largest exponents (of grad_loss, of the inverse scales) of kept rows
+    const float* grad_loss;   // null, or for `most`: per CTA what Scales::h is the largest of
     uint64_t grad_stride;
-    int2* most;
+    int* most;
     uint32_t* count;          // kept tokens
     uint32_t* splits;         // null, or for SumPlan::parts()
     SumPlan sum;
@@ -191,7 +195,7 @@ __device__ __forceinline__ uint2 count_kept(const GatherArgs& p, uint32_t first,
 // Gathers the kept rows of h in the order of the tokens, and zeros behind them up to a multiple of kRowPad.  Every CTA
 // counts all targets itself: that takes 64 KB from L2 for 8192 tokens.
 template <typename T>
-__device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
+__device__ __forceinline__ void gather_rows(const GatherArgs& p, int* tops) {
     __shared__ uint2 shared[8];
     const uint32_t first = blockIdx.x * p.per_block, end = min(first + p.per_block, p.tokens);   // (none in the last CTAs of few tokens)
     const uint2 c = count_kept(p, first, shared);
@@ -202,7 +206,7 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
         if (p.splits) *p.splits = p.sum.parts(c.y);
     }
     uint32_t before = c.x;
-    int2 most = make_int2(kLeastExponent, -126);
+    int most = kLeastExponent - 126;
     for (uint32_t t0 = first; t0 < end; t0 += 32) {
         const uint32_t t = t0 + lane;
         const int64_t y = t < end ? target_of(p, t) : p.ignore;
@@ -222,10 +226,10 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
             left &= left - 1;
             if (i % 8 != warp) continue;
             const T* src = static_cast<const T*>(p.h) + uint64_t(t0 + at) * p.h_stride;
-            most.y = max(most.y, copy_row(src, p.width, p.to, before + i, lane));
+            const int inverse = copy_row(src, p.width, p.to, before + i, lane);
             if (p.grad_loss) {
-                const float a = fabsf(p.grad_loss[(t0 + at) * p.grad_stride]);
-                if (a < INFINITY) most.x = max(most.x, exponent(a));
+                const float a = p.grad_loss[(t0 + at) * p.grad_stride];
+                if (fabsf(a) < INFINITY) most = max(most, grad_exponent(a) + inverse);
             }
         }
         before += __popc(kept);
@@ -240,7 +244,7 @@ __device__ __forceinline__ void gather_rows(const GatherArgs& p, int2* tops) {
         if (lane == 0) tops[warp] = most;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int i = 1; i < 8; ++i) most = make_int2(max(most.x, tops[i].x), max(most.y, tops[i].y));
+            for (int i = 1; i < 8; ++i) most = max(most, tops[i]);
             p.most[blockIdx.x] = most;
         }
     }
@@ -256,16 +260,16 @@ struct PackArgs {
 
 // W as rows that TMA can read, by `blocks` CTAs.
 template <typename T>
-__device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, int2* tops) {
+__device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, int* tops) {
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     int most = -126;
     for (uint32_t r = block * 8 + warp; r < p.rows; r += p.blocks * 8)
         most = max(most, copy_row(static_cast<const T*>(p.w) + uint64_t(r) * p.stride, p.width, p.to, r, lane));
     if (!p.most) return;
-    if (lane == 0) tops[warp].x = most;
+    if (lane == 0) tops[warp] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) most = max(most, tops[i].x);
+        for (int i = 1; i < 8; ++i) most = max(most, tops[i]);
         p.most[block] = most;
     }
 }
@@ -274,47 +278,47 @@ __device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, int
 // 509 tokens on 10007 x 451, loss and gradient 117 us, 121 with two.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_operands(const __grid_constant__ GatherArgs h, const __grid_constant__ PackArgs w) {
-    __shared__ int2 tops[8];
+    __shared__ int tops[8];
     wait_previous();
     if (blockIdx.x < h.blocks) gather_rows<T>(h, tops);
     else pack_rows<T>(w, blockIdx.x - h.blocks, tops);
 }
 
 struct EvenArgs {
-    const int2* most_h;
-    const int* most_w;
+    const int *most_h, *most_w;
     uint32_t n_h, n_w;
     Scales* scales;
     const uint32_t* count;
+    const int* token;
+    const float* grad_loss;
+    uint64_t grad_stride;
     Planes from, to;          // to.hi: null if not needed
 };
 
-// The scales of a call, and the gathered h once more with one scale for all rows (zeros behind the kept rows again).
+// The scales of a call, and grad_loss_t h_t of the gathered rows with one scale for all (zeros behind the kept rows again).
 __global__ void __launch_bounds__(256) k_ce_even(const __grid_constant__ EvenArgs p) {
-    __shared__ int tops[3];
-    if (threadIdx.x < 3) tops[threadIdx.x] = -126;
+    __shared__ int tops[2];
+    if (threadIdx.x < 2) tops[threadIdx.x] = kLeastExponent - 126;
     __syncthreads();
     wait_previous();
-    int grad = -126, h = -126, w = -126;
-    for (uint32_t i = threadIdx.x; i < p.n_h; i += 256) {
-        grad = max(grad, p.most_h[i].x);
-        h = max(h, p.most_h[i].y);
-    }
+    int h = kLeastExponent - 126, w = -126;
+    for (uint32_t i = threadIdx.x; i < p.n_h; i += 256) h = max(h, p.most_h[i]);
     if (blockIdx.x == 0)
         for (uint32_t i = threadIdx.x; i < p.n_w; i += 256) w = max(w, p.most_w[i]);
-    atomicMax(&tops[0], grad);
-    atomicMax(&tops[1], h);
-    atomicMax(&tops[2], w);
+    atomicMax(&tops[0], h);
+    atomicMax(&tops[1], w);
     __syncthreads();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.scales = Scales{tops[0], tops[1], tops[2]};
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.scales = Scales{tops[0], tops[1]};
     if (!p.to.hi) return;
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, count = *p.count;
     const uint32_t pad = (count + kRowPad - 1) / kRowPad * kRowPad;
     for (uint32_t r = blockIdx.x * 8 + warp; r < pad; r += gridDim.x * 8) {
-        float by = 0.f;
+        float a = 0.f, by = 0.f;   // a: below 2, and half of it by the scale
         if (r < count) {
-            const int e = static_cast<int>(__float_as_uint(p.from.inverse[r]) >> 23) - 127 - tops[1];
-            by = power(e < -126 ? -126 : e);
+            a = p.grad_loss[p.token[r] * p.grad_stride];
+            const int own = grad_exponent(a), e = own + static_cast<int>(__float_as_uint(p.from.inverse[r]) >> 23) - 127 - tops[0] - 1;
+            a *= power(-own);
+            by = power(e < -126 ? -126 : e > 0 ? 0 : e);   // (> 0: of a that is not finite)
         }
         for (uint32_t k = lane * 8; k < p.to.ld; k += 256) {
             const uint64_t at = uint64_t(r) * p.to.ld + k;
@@ -322,7 +326,7 @@ __global__ void __launch_bounds__(256) k_ce_even(const __grid_constant__ EvenArg
             float v[8];
             unpack8<__half, true>(hi, lo, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= by;
+            for (int i = 0; i < 8; ++i) v[i] = v[i] * a * by;
             const uint4 e = pack8<__half>(v);
             *reinterpret_cast<uint4*>(p.to.hi + at) = e;
             *reinterpret_cast<uint4*>(p.to.lo + at) = rest8<__half>(v, e);
@@ -466,9 +470,9 @@ struct EpiGrad {
         if (in) {
             const uint32_t tok = token[row + buf.lane];
             y = static_cast<uint32_t>(target[row + buf.lane]) - v0;
-            a = grad_loss[tok * grad_stride];
             ref = PAIR ? lse[tok] : lse[tok] * kLog2e;
             if constexpr (PAIR) by = h_inverse[row + buf.lane];
+            else a = grad_loss[tok * grad_stride];
         }
         float left[2] = {};
 #pragma unroll
@@ -528,11 +532,10 @@ struct EpiGrad {
                         return rest8<__half>(x, pack8<__half>(x));
                     });
                 };
-                // |G_tv| <= |grad_loss_t|: below f16's range with its exponent taken out
-                const Scales sc = *scales;
-                const float own = a * power(kTopExponent - exponent(a)), all = a * power(kTopExponent - sc.grad), down = power(-sc.w);
-                if (for_h) both(0, [&](int k) { return v[k] * own * (iw[k] * down); });
-                if (for_w) both(2, [&](int k) { return v[k] * all; });
+                // |G_tv| <= 1: with 2^kTopExponent below f16's range
+                const float down = power(-scales->w), up = power(kTopExponent);
+                if (for_h) both(0, [&](int k) { return v[k] * up * (iw[k] * down); });
+                if (for_w) both(2, [&](int k) { return v[k] * up; });
             }
         }
         if (!PAIR && in && for_h && col < columns)
@@ -592,7 +595,7 @@ struct EpiWeight {
     __device__ __forceinline__ bool tile(const Tile&, uint32_t row, uint32_t col, const Columns& acc, bool empty, WarpBuffer& buf) const {
         constexpr bool kPair = sizeof(T) == 4;
         constexpr int kBox = 128 / sizeof(T), kPer = 16 / sizeof(T);
-        const int e = kPair ? scales->grad + scales->h - kTopExponent : 0;
+        const int e = kPair ? scales->h + 1 - kTopExponent : 0;
         const float by[2] = {power(e / 2), power(e - e / 2)};
 #pragma unroll
         for (int c = 0; c < COLUMNS; c += kBox) {
@@ -698,8 +701,10 @@ __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ Scat
             }
         } else {
             if (row >= 0) {
-                const int e = exponent(p.grad_loss[t * p.grad_stride]) + p.scales->w - kTopExponent;
-                v = make_float4(times_power(v.x, e), times_power(v.y, e), times_power(v.z, e), times_power(v.w, e));
+                float a = p.grad_loss[t * p.grad_stride];
+                const int own = grad_exponent(a), e = own + p.scales->w - kTopExponent;
+                a *= power(-own);
+                v = make_float4(times_power(v.x * a, e), times_power(v.y * a, e), times_power(v.z * a, e), times_power(v.w * a, e));
             }
         }
         __align__(16) T out[4] = {round_to<T>(v.x), round_to<T>(v.y), round_to<T>(v.z), round_to<T>(v.w)};
@@ -751,15 +756,14 @@ struct Plan {
     int tile_v;               // columns of a tile of the logits
     uint32_t groups;          // of the vocabulary's columns, each with a partial result of the loss
     bool pair, pack;          // 32-bit operands; W has to be laid out for TMA
-    Planes h, w, even;        // even: h with one scale for all rows
+    Planes h, w, even;        // even: grad_loss_t h_t with one scale for all rows
     uint16_t* g[4];           // hi; hi and lo for dh, for dW
     uint32_t* count;          // kept tokens; parts of dh
     int *target, *token, *row;
     long long* rest;
     float2* partial;
     float* target_logit;
-    int2* most_h;
-    int* most_w;
+    int *most_h, *most_w;
     Scales* scales;
     uint32_t piece, pieces;   // vocabulary rows of a piece of G
     SumPlan parts;            // of dh
@@ -808,7 +812,7 @@ Plan make_plan(const dsm_linear_ce& p, bool grad, void* workspace) {
         r.w.lo = c.take<uint16_t>(uint64_t(p.vocab) * r.w.ld);
         r.h.inverse = c.take<float>(r.rows);
         r.w.inverse = c.take<float>(round_up(p.vocab, kPieceUnit));
-        r.most_h = c.take<int2>(kGatherBlocks);
+        r.most_h = c.take<int>(kGatherBlocks);
         r.most_w = c.take<int>(kPackBlocks);
         r.scales = c.take<Scales>(1);
     }
@@ -906,7 +910,7 @@ cudaError_t gather(const dsm_linear_ce& p, const Plan& r, const float* grad_loss
     Planes even = r.even;
     if (!for_w) even.hi = even.lo = nullptr;
     return launch_grid(k_ce_even, dim3(for_w ? a.blocks : 1), 256, 0, s,
-                       EvenArgs{r.most_h, r.most_w, a.blocks, k.blocks, r.scales, r.count, r.h, even});
+                       EvenArgs{r.most_h, r.most_w, a.blocks, k.blocks, r.scales, r.count, r.token, grad_loss, grad_stride, r.h, even});
 }
 
 // Arguments that both calls check against the device.

@@ -264,3 +264,34 @@ def test_long_sums_of_one_sign(width, vocab, tokens):
     _, lse = dsm.linear_cross_entropy(h, w, y)
     want = torch.logsumexp(h.double() @ w.double().T, 1)
     assert abs(float(((lse.double() - want) / want).mean())) < 16 * 2.0 ** -24
+
+
+# ---- f32 gradients of tokens that count for very different amounts ----------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [17, 100, 300])
+@pytest.mark.parametrize("spread", [0, 15, 25, 35, 60])
+def test_grad_loss_of_very_different_sizes(spread, tokens):
+    """Tokens whose loss counts for little, beside sure ones that count for much and touch few rows of dW: the other rows are
+    the small tokens' alone.  Bounds as in rows_within_bounds(), but absolutely only 2^-39 of each token's own grad_loss_t h_t
+    (and not more than its G there), and 2^-39 of the largest value of grad_loss_t h_t times G."""
+    h, w, y, a = problem(tokens, 1030, 96, F32, lean=4.0)
+    big = torch.arange(tokens, device="cuda") % 4 == 0
+    y[big] %= 10
+    w[:10] *= 20
+    h[big] = (h + 3 * w[y])[big]
+    a[~big] *= 2.0 ** -spread
+    h64, w64, a64 = h.double(), w.double(), a.double()
+    z = h64 @ w64.T
+    p = torch.softmax(z, 1)
+    size = torch.maximum((h64.abs() @ w64.abs().T).amax(1), torch.logsumexp(z, 1).abs()).clamp_min(1.0)
+    q = p.clone()
+    q[torch.arange(tokens, device="cuda"), y] -= 1
+    dh, dw = a64[:, None] * (q @ w64), q.T @ (a64[:, None] * h64)
+    off = p * (2.0 ** -20 * size)[:, None] + 2.0 ** -21 * q.abs()
+    ah = a64 * h64.norm(dim=1)
+    bound_h = a64 * (off @ w64.norm(dim=1) + 2.0 ** -39 * len(w) * 96 ** 0.5 * float(w64.abs().max()))
+    bound_w = (off + q.abs().clamp_max(2.0 ** -39)).T @ ah + 2.0 ** -39 * 96 ** 0.5 * float((a64[:, None] * h64).abs().max()) * q.abs().sum(0)
+    _, lse = dsm.linear_cross_entropy(h, w, y)
+    got_h, got_w = dsm.linear_cross_entropy_grad(h, w, y, lse, a)
+    assert bool(((got_h.double() - dh).norm(dim=1) <= bound_h).all())
+    assert bool(((got_w.double() - dw).norm(dim=1) <= bound_w).all())
