@@ -615,7 +615,7 @@ struct EpiWeight {
                     r = pack8<T>(v + kPer * j);
                 sts128(buf.at(j), empty ? uint4{} : r);
             }
-            if (tma) {
+            if (tma && ends_whole<T>(col + c + kBox, width)) {
                 if (buf.written()) {
                     tma_store(&to, buf.addr, col + c, row, 0);
                     tma_store_commit();

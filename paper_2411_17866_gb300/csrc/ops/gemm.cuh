@@ -154,6 +154,13 @@ struct WarpBuffer {
     }
 };
 
+// Whether TMA may store a box that ends at column `end` of rows of `cols` columns of the caller's: it writes whole pieces of 16
+// bytes, the one with a row's last column too, and what lies behind that is not the operator's.
+template <typename T>
+__device__ __forceinline__ bool ends_whole(uint32_t end, uint32_t cols) {
+    return end <= cols || cols % (16 / sizeof(T)) == 0;
+}
+
 // Stores every STEP'th of a buffer's 32 rows of 64 16-bit values, from row `first` on, two values at a time.  ODD: rows that
 // start in the middle of a word; the first and the last value are then stored alone.
 template <bool ODD, int STEP>

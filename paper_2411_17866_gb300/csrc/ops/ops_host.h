@@ -75,7 +75,8 @@ int device_of_call(const char* func, int* dev, int* sms);
 enum class Elem { f16, bf16, f32 };
 
 // A 3-D tensor map with the 128-byte swizzle: (x, y, z) of the sizes nx, ny, nz; rows of `ld` elements, planes of
-// `plane` elements; a box of 128 bytes x rows x 1.  What lies outside reads as zero and is not written.
+// `plane` elements; a box of 128 bytes x rows x 1.  What lies outside reads as zero and is not written (but in pieces of
+// 16 bytes: see tma_store).
 int make_map(const char* func, CUtensorMap* map, const void* base, uint64_t nx, uint64_t ny, uint64_t nz, uint64_t ld,
              uint64_t plane, uint32_t rows, Elem type);
 // The same without a swizzle and with boxes of 64 bytes x rows x 1.

@@ -345,8 +345,8 @@ struct EpiSquare {
     }
 };
 
-// X <- a X + B X (or X B); the last step's goes out instead, times scale: by TMA, or by plain stores with neighbouring
-// threads on neighbouring columns or rows.
+// X <- a X + B X (or X B); the last step's goes out instead, times scale: by TMA (but for the ragged end of rows), or by
+// plain stores with neighbouring threads on neighbouring columns or rows.
 enum class Out { none, tma, columns, rows };
 template <typename T>
 struct EpiApply {
@@ -446,7 +446,7 @@ struct EpiApply {
                 else r = pack8<T>(v + 8 * j);
                 sts128(buf.at(j % 8) + j / 8 * 4096 + half, r);
             }
-            if (mode == Out::tma) {
+            if (mode == Out::tma && ends_whole<T>(col + x + 64, cols)) {
                 if (buf.written()) {
                     tma_store(&step.map, buf.addr + half, col + x, row, t.batch);
                     if constexpr (sizeof(T) == 4) tma_store(&step.map, buf.addr + 4096, col + x + 32, row, t.batch);

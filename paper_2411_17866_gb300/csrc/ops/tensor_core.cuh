@@ -114,7 +114,8 @@ __device__ __forceinline__ void tma_fetch(uint32_t dst, const CUtensorMap* map, 
     tma_load<1>(dst, map, bar, x, y, z);
 }
 
-// Writes (or adds, f32) a box from shared memory.  What lies outside the map is left out.
+// Writes (or adds, f32) a box from shared memory.  What lies outside the map is left out, but for the rest of the 16 bytes with a
+// row's last column.
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src),
                  "r"(x), "r"(y), "r"(z)
