@@ -725,10 +725,13 @@ __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ Scat
 // Tiles of the products: 256 columns, or 128 where the sums are held in registers (32-bit operands).
 template <bool PAIR>
 constexpr int kTileN = PAIR ? 128 : 256;
-// k between two additions to sums in registers, of 32-bit operands: for dh and dW 64, which keeps a row whose value is a single
-// product (dW's of a target that occurs once) to 3e-7; 128 took it to 7e-7 (loss and gradient of 509 tokens on 10007 x 451: 123.5
-// and 122.9 us).
-constexpr uint32_t kChunkLogits = 128, kChunkGrad = 64;
+// k between two additions to sums in registers.  Logits: 512 with 16-bit operands, if there are more at all (what the
+// accumulators cut off of 1600 k reaches 1e-6 of the loss), 128 with 32-bit ones.  dh and dW of 32-bit operands: 64, which keeps
+// a row whose value is a single product (dW's of a target that occurs once) to 3e-7; 128 took it to 7e-7 (loss and gradient
+// of 509 tokens on 10007 x 451: 123.5 and 122.9 us).
+constexpr uint32_t kUnchunked = 512, kChunkGrad = 64;
+template <bool PAIR>
+constexpr uint32_t kChunkLogits = PAIR ? 128 : 512;
 constexpr int kPairRows = 128;                   // up to so many tokens a CTA multiplies by itself (CG = 1), else pairs do
 constexpr int kPieceUnit = 256;                  // pieces of the vocabulary come in multiples of this
 constexpr uint64_t kPieceBytes = 256ull << 20;   // most bytes of a piece of G with 16-bit operands, half of them with 32-bit ones
@@ -1037,10 +1040,9 @@ int forward(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_t* s
     w.m_count = r.count;
     EpiLoss<PAIR> e{r.count, r.target, r.h.inverse, r.w.inverse, r.partial, r.target_logit, p.vocab, r.rows};
     const uint64_t tiles = uint64_t(w.tiles_m) * w.tiles_n;
-    // Sums in registers beyond 512 k: what the accumulators cut off reaches 1e-6 of the loss (width 1600).
     cudaError_t err;
-    if (PAIR || w.k > 512) err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits : 512, !PAIR, false, false>(maps, w, e, tiles, sms, s);
-    else err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits : 0, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BN, kTerms, kChunkLogits<PAIR>, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    else err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits<PAIR> : 0, !PAIR, false, false>(maps, w, e, tiles, sms, s);
     return err == cudaSuccess ? DSM_OK : cuda_fail(func, err, "launch the logits");
 }
 
@@ -1083,8 +1085,11 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         w.tiles_n = ceil_div(count, BV);
         w.k = p.width;
         w.m_count = r.count;
-        err = launch_gemm<CG, BV, kTerms, PAIR ? kChunkLogits : 0, !PAIR, false, false>(Maps{{hk[0], hk[1]}, {wk[0], wk[1]}}, w, eg,
-                                                                    uint64_t(w.tiles_m) * w.tiles_n, sms, s);
+        const Maps logits{{hk[0], hk[1]}, {wk[0], wk[1]}};
+        const uint64_t tiles = uint64_t(w.tiles_m) * w.tiles_n;
+        // (as the loss forms them: what is cut off then cancels against lse, and a sure token's p - 1 is right)
+        if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BV, kTerms, kChunkLogits<PAIR>, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
+        else err = launch_gemm<CG, BV, kTerms, PAIR ? kChunkLogits<PAIR> : 0, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the logits' gradient");
         // its contribution to dh
         w.tiles_n = ceil_div(p.width, BN);

@@ -295,3 +295,14 @@ def test_grad_loss_of_very_different_sizes(spread, tokens):
     got_h, got_w = dsm.linear_cross_entropy_grad(h, w, y, lse, a)
     assert bool(((got_h.double() - dh).norm(dim=1) <= bound_h).all())
     assert bool(((got_w.double() - dw).norm(dim=1) <= bound_w).all())
+
+
+# ---- sure tokens ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width", [(3, 20, 1600), (8, 20, 1600), (8, 20, 520), (17, 20, 1100), (60, 90, 1900), (140, 20, 1600),
+                                                (300, 1030, 4096)])
+def test_tokens_that_are_sure(tokens, vocab, width, dtype):
+    """Logits that are nearly all of lse: what is left of p - 1 shows whether the gradient forms them as the loss did."""
+    for _ in range(30 if tokens < 100 else 5):
+        check(*problem(tokens, vocab, width, dtype, 0.5 if tokens > 3 else 0.0, lean=20.0 if width < 4000 else 6.0))
