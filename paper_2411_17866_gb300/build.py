@@ -51,9 +51,11 @@ def _run(cmd, verbose):
 def build(verbose: bool = False, fmad: bool = False, out: str = LIB) -> str:
     """Compile and link libdsm.so (to ``out``); returns its path.
 
-    fmad=True builds with nvcc's default multiply-add contraction; the method's
+    fmad=True builds with nvcc's default multiply-add contraction; the rounds'
     arithmetic is written with explicit round-to-nearest intrinsics, which are
-    never contracted, so both builds give identical results (a GPU test checks).
+    never contracted, so both builds give identical rounds (a GPU test checks).
+    The operators' plain products and sums may be contracted, and their last
+    bits differ.
     """
     objdir = os.path.join(BUILD, "fmad" if fmad else "nofmad")
     os.makedirs(objdir, exist_ok=True)

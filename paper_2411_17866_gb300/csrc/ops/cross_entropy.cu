@@ -725,13 +725,14 @@ __global__ void __launch_bounds__(256) k_ce_scatter(const __grid_constant__ Scat
 // Tiles of the products: 256 columns, or 128 where the sums are held in registers (32-bit operands).
 template <bool PAIR>
 constexpr int kTileN = PAIR ? 128 : 256;
-// k between two additions to sums in registers.  Logits: 512 with 16-bit operands, if there are more at all (what the
-// accumulators cut off of 1600 k reaches 1e-6 of the loss), 128 with 32-bit ones.  dh and dW of 32-bit operands: 64, which keeps
-// a row whose value is a single product (dW's of a target that occurs once) to 3e-7; 128 took it to 7e-7 (loss and gradient
-// of 509 tokens on 10007 x 451: 123.5 and 122.9 us).
-constexpr uint32_t kUnchunked = 512, kChunkGrad = 64;
+// k between two additions to sums in registers.  16-bit operands: 512 in the logits, if there are more at all (what the
+// accumulators cut off of 1600 k reaches 1e-6 of the loss).  32-bit ones: 64 in all products, one stage, whose terms with lo
+// come first, while the sum is small.  Then errors are below those of f32 arithmetic (loss, lse, dh and dW of 509 tokens on
+// 10007 x 451: 1.4e-7, 8e-8, 2.9e-7, 2.8e-7, and twice that with 128 in the logits); loss and gradient of these take 127.5 us
+// and 125.5, of 1024 tokens on 50257 x 768 776 and 733.
+constexpr uint32_t kUnchunked = 512;
 template <bool PAIR>
-constexpr uint32_t kChunkLogits = PAIR ? 128 : 512;
+constexpr uint32_t kChunk = PAIR ? 64 : 512;
 constexpr int kPairRows = 128;                   // up to so many tokens a CTA multiplies by itself (CG = 1), else pairs do
 constexpr int kPieceUnit = 256;                  // pieces of the vocabulary come in multiples of this
 constexpr uint64_t kPieceBytes = 256ull << 20;   // most bytes of a piece of G with 16-bit operands, half of them with 32-bit ones
@@ -1041,8 +1042,8 @@ int forward(const char* func, const dsm_linear_ce& p, const Plan& r, uint32_t* s
     EpiLoss<PAIR> e{r.count, r.target, r.h.inverse, r.w.inverse, r.partial, r.target_logit, p.vocab, r.rows};
     const uint64_t tiles = uint64_t(w.tiles_m) * w.tiles_n;
     cudaError_t err;
-    if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BN, kTerms, kChunkLogits<PAIR>, !PAIR, false, false>(maps, w, e, tiles, sms, s);
-    else err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkLogits<PAIR> : 0, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BN, kTerms, kChunk<PAIR>, !PAIR, false, false>(maps, w, e, tiles, sms, s);
+    else err = launch_gemm<CG, BN, kTerms, PAIR ? kChunk<PAIR> : 0, !PAIR, false, false>(maps, w, e, tiles, sms, s);
     return err == cudaSuccess ? DSM_OK : cuda_fail(func, err, "launch the logits");
 }
 
@@ -1088,8 +1089,8 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         const Maps logits{{hk[0], hk[1]}, {wk[0], wk[1]}};
         const uint64_t tiles = uint64_t(w.tiles_m) * w.tiles_n;
         // (as the loss forms them: what is cut off then cancels against lse, and a sure token's p - 1 is right)
-        if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BV, kTerms, kChunkLogits<PAIR>, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
-        else err = launch_gemm<CG, BV, kTerms, PAIR ? kChunkLogits<PAIR> : 0, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
+        if (PAIR || w.k > kUnchunked) err = launch_gemm<CG, BV, kTerms, kChunk<PAIR>, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
+        else err = launch_gemm<CG, BV, kTerms, PAIR ? kChunk<PAIR> : 0, !PAIR, false, false>(logits, w, eg, tiles, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the logits' gradient");
         // its contribution to dh
         w.tiles_n = ceil_div(p.width, BN);
@@ -1097,7 +1098,7 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         w.split_count = r.count + 1;
         w.n_fast = 1;
         es.add = i > 0;
-        if (dh) err = launch_gemm<CG, BN, kTerms, PAIR ? kChunkGrad : 0, !PAIR, false, true>(Maps{{gk[0], gk[1]}, {wm[0], wm[1]}}, w, es,
+        if (dh) err = launch_gemm<CG, BN, kTerms, PAIR ? kChunk<PAIR> : 0, !PAIR, false, true>(Maps{{gk[0], gk[1]}, {wm[0], wm[1]}}, w, es,
                                                                             ~uint64_t(0), sms, s);   // (all SMs)
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the gradient of h");
         if (!dw) continue;
@@ -1113,7 +1114,7 @@ int backward(const char* func, const dsm_linear_ce& p, const Plan& r, const floa
         ew.tma = mappable(out, static_cast<int64_t>(dw_stride), 16, count, 1, sizeof(T));
         if (ew.tma)
             if (int rc = make_map(func, &ew.to, out, p.width, count, 1, dw_stride, 0, 32, kOut)) return rc;
-        err = launch_gemm<2, BN, kTerms, PAIR ? kChunkGrad : 0, !PAIR, true, true>(Maps{{gm[0], gm[1]}, {hm[0], hm[1]}}, w, ew,
+        err = launch_gemm<2, BN, kTerms, PAIR ? kChunk<PAIR> : 0, !PAIR, true, true>(Maps{{gm[0], gm[1]}, {hm[0], hm[1]}}, w, ew,
                                                                   uint64_t(w.tiles_m) * w.tiles_n, sms, s);
         if (err != cudaSuccess) return cuda_fail(func, err, "launch the gradient of W");
     }

@@ -306,3 +306,17 @@ def test_tokens_that_are_sure(tokens, vocab, width, dtype):
     """Logits that are nearly all of lse: what is left of p - 1 shows whether the gradient forms them as the loss did."""
     for _ in range(30 if tokens < 100 else 5):
         check(*problem(tokens, vocab, width, dtype, 0.5 if tokens > 3 else 0.0, lean=20.0 if width < 4000 else 6.0))
+
+
+@pytest.mark.parametrize("tokens", [60, 200])
+@pytest.mark.parametrize("vocab", [700, 10007])
+@pytest.mark.parametrize("width", [256, 768, 1024, 1600])
+def test_long_f32_sums_of_one_sign(width, vocab, tokens):
+    """f32 operands: sums leave the accumulators every 64 k, within which the four large additions of 16 k cut off 2^-24 of the sum
+    so far on average, 2.5 * 2^-24 of a whole (1/4 + 2/4 + 3/4 + 1); those before, with lo, nearly nothing."""
+    h = torch.rand(tokens, width, device="cuda")
+    w = torch.rand(vocab, width, device="cuda") * (160 / width)
+    y = torch.randint(0, vocab, (tokens,), device="cuda")
+    _, lse = dsm.linear_cross_entropy(h, w, y)
+    want = torch.logsumexp(h.double() @ w.double().T, 1)
+    assert abs(float(((lse.double() - want) / want).mean())) < 4 * 2.0 ** -24
