@@ -275,7 +275,7 @@ __device__ __forceinline__ void pack_rows(const PackArgs& p, uint32_t block, int
 }
 
 // The operands of the products: the gathered h and, where W has to be laid out, in further CTAs W.  (One launch for both: f32,
-// 509 tokens on 10007 x 451, loss and gradient 117 us, 121 with two.)
+// 509 tokens on 10007 x 451, loss and gradient take 4 us less than with two.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_operands(const __grid_constant__ GatherArgs h, const __grid_constant__ PackArgs w) {
     __shared__ int tops[8];
@@ -741,8 +741,8 @@ constexpr uint32_t kGatherBlocks = 512, kPackBlocks = 2048;   // most CTAs of th
 
 // Few tokens go another way (few_tokens.cuh), if their rows of h fit into shared memory: up to 4 with 16-bit operands, up
 // to 16 with 32-bit ones, which the products would have to lay out first.  This way and by the products, vocabulary 50257 x
-// 768: loss of 4 tokens bf16 25 and 31 us, of 8 35 and 30, of 16 f32 63 and 113, of 32 114 and 110; loss and gradient of 4
-// tokens bf16 86 and 113 us, of 8 129 and 110, of 16 f32 209 and 319.  (Where W has to be laid out because of its alignment,
+// 768: loss of 4 tokens bf16 24 and 28 us, of 8 35 and 27, of 16 f32 61 and 87, of 32 114 and 88; loss and gradient of 4
+// tokens bf16 83 and 89 us, of 8 129 and 89, of 16 f32 210 and 259.  (Where W has to be laid out because of its alignment,
 // x 1102, 5 to 8 tokens bf16: loss 72 and 83, loss and gradient 232 and 221: no rule of its own.)
 constexpr uint32_t kFew16 = 4, kFew32 = 16, kFewSmem = 208 * 1024;
 int few_size(const dsm_linear_ce& p) {   // tokens of the kernels' variant; 0: not few

@@ -70,7 +70,7 @@ struct Shape {
     static constexpr uint32_t kStages = kFit < 12 ? kFit : 12;
     static constexpr uint32_t kSmem = kStages * kStage + kBuffers + 2048;           // 1024 for alignment, 1024 for barriers
     // Accumulators: with sums in registers as many as tensor memory holds (they are small turns: while a tile is stored the
-    // next one's first ones are multiplied; 1024 tokens on 50257 x 768 f32: loss 206 us with two, 188 with four).
+    // next one's first ones are multiplied; 1024 tokens on 50257 x 768 f32: loss 218 us with two, 204 with four).
     static constexpr uint32_t kAcc = CHUNKED && BN == 128 ? 4 : 2;
     static constexpr uint32_t kColumns = kAcc * BN;                                 // of tensor memory
     static_assert(BN == 64 || BN == 128 || BN == 256, "tile shape");
