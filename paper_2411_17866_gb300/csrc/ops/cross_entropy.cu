@@ -15,14 +15,15 @@
 // Numbers.  16-bit operands are multiplied as they are (bf16, f32 accumulators), G is rounded to bf16.  A token's G adds up
 // to zero, so what W's rows have in common drops out of dh; of the rounded G a rest s_t is left, and dh takes
 // G W - s_t W_y, which puts the rest on the target and with it back to zero.  (All rows of W with a common part that moves
-// the logits to -120: dh was off by 6.5 %, and is by 0.3 %.)  32-bit operands
-// are kept as pairs hi + lo of f16 (22 bits) and multiplied in three terms.  Every row of h and of W is scaled by a power
-// of two of its own so that its largest value lies just below f16's range.  G is kept without
-// grad_loss, p_tv - [v = y_t], and twice: for dh with the scales of W's rows, which its product sums over (grad_loss_t comes
-// last), and for dW as it is, against grad_loss_t h_t under one scale for all.  So neither a row of W nor a token sets the
-// precision of another's gradient: G and grad_loss_t h_t keep 22 bits down to 2^-17 of their largest value, and 2^-39 of
-// that as an absolute error below.  (G once, with both scales folded in: rows of W or h that are zero, or much smaller than the
-// others, cost dh and dW up to 31 bits.)  Statistics, lse and the sums for dh are in f32.
+// the logits to -120: dh was off by 6.5 %, and is by 0.3 %.)
+//
+// 32-bit operands are kept as pairs hi + lo of f16 (22 bits) and multiplied in three terms.  Every row of h and of W is scaled
+// by a power of two of its own so that its largest value lies just below f16's range.  G is kept without grad_loss,
+// p_tv - [v = y_t], and twice: for dh with the scales of W's rows, which its product sums over (grad_loss_t comes last), and
+// for dW as it is, against grad_loss_t h_t under one scale for all.  So neither a row of W nor a token sets the precision of
+// another's gradient: G and grad_loss_t h_t keep 22 bits down to 2^-17 of their largest value, and 2^-39 of that as an
+// absolute error below.  (G once, with both scales folded in: rows of W or h that are zero, or much smaller than the others,
+// cost dh and dW up to 31 bits.)  Statistics, lse and the sums for dh are in f32.
 #include <type_traits>
 
 #include "few_tokens.cuh"
@@ -444,7 +445,8 @@ __global__ void __launch_bounds__(1024) k_ce_join(const __grid_constant__ JoinAr
     p.loss[p.token[r]] = lse - p.target_logit[r];
 }
 
-// Sums over a row of G are kept as whole numbers, so that their order does not matter: |grad_loss| is below 2^(kRestBits + 1).
+// What a row of the rounded G adds up to is kept as a whole number, so that the order of the additions does not matter: in units
+// of 2^-kRestBits times grad_loss' power of two, so that grad_loss itself is below 2^(kRestBits + 1).
 constexpr int kRestBits = 40;
 
 // A piece of G from the logits.  Rows beyond the kept ones are written as zeros: the products over G read them.  With PAIR
@@ -457,7 +459,7 @@ struct EpiGrad {
     const int *target, *token;
     const float *lse, *grad_loss, *h_inverse, *w_inverse;
     const Scales* scales;
-    long long* rest;          // 16-bit: per row what its rounded G adds up to, in units of 2^-kRestBits of a power of two
+    long long* rest;          // 16-bit: per row what its rounded G adds up to, see kRestBits
     uint64_t grad_stride;
     uint32_t v0, columns;     // the piece's first vocabulary row and their number
     int for_h, for_w;         // which of G's forms are needed
